@@ -16,7 +16,8 @@
  * and jitdb_cache_* (a cache of tables keyed by the parent array), jitdb_schedule_typed and
  * jitdb_treelstm_forward_typed (the table keyed by depth and signature, one cell per signature),
  * jitdb_treelstm_pack and jitdb_treelstm_forward_packed (weights packed once for many calls),
- * jitdb_treelstm_forward_train and jitdb_treelstm_backward (the training step).
+ * jitdb_treelstm_forward_train and jitdb_treelstm_backward (the training step), jitdb_layernorm_*,
+ * jitdb_dropout and jitdb_softmax_xent_* (what a training step does between the two).
  *
  * Conventions
  *   - Every function returns JITDB_OK (0) or a negative jitdb_status.  Nothing
@@ -437,6 +438,84 @@ int jitdb_treelstm_backward(const void *x, const void *W, const void *U,
                             void *workspace, size_t workspace_bytes, void *hip_stream);
 
 /*
+ * The head of a training step: what stands between the h of jitdb_treelstm_forward_train and the gh that
+ * jitdb_treelstm_backward takes.  All calls are asynchronous on `hip_stream`, allocate nothing, wait for
+ * nothing and may be recorded into a HIP graph.  Rows are the nodes of a forest (or any rows).  Pointers
+ * need the alignment of their elements only, workspaces 256 bytes.  A sum's order depends on the sizes (and,
+ * for the loss, on which rows have a label), never on timing: equal calls give equal bits.
+ *
+ * Dropout:  y_i = x_i / (1 - p) where element i is kept, else 0 (whatever x_i is).
+ * Element i is kept where half i % 2 (the low half first) of the 64-bit word
+ *     mix64(mix64(seed) + (first + i / 2) * 0x9E3779B97F4A7C15)   mod 2^64
+ * is at least p * 2^32, with mix64 as above.  No mask is stored: the same call on the cotangent of y gives
+ * that of x.  A call on n elements uses (n + 1) / 2 words; the next call starts behind them (or uses another seed).
+ *
+ *   x, y    dev [n] in dtype elements; y may be x
+ *   p       in [0, 1]
+ *   state   dev [2] uint64: seed, first word.  Read by the kernel, so that a replayed graph draws new
+ *           masks where the program changes it in between; never written
+ */
+int jitdb_dropout(const void *x, int64_t n, jitdb_dtype dtype, float p, const uint64_t *state,
+                  void *y, void *hip_stream);
+
+/*
+ * Layer norm of each row, with dropout behind it if p > 0 (element i = row * H + column of the definition above):
+ *     mean = sum x / H   rstd = 1 / sqrt(sum (x - mean)^2 / H + eps)   y = D((x - mean) rstd gamma + beta)
+ *
+ *   x, y         dev [n_rows, H] in dtype elements; y may be x
+ *   gamma, beta  dev [H] fp32
+ *   mean, rstd   dev [n_rows] fp32, out, or NULL where no backward pass follows
+ *   state        as above; may be NULL if p == 0
+ * 1 <= H <= 16384, eps >= 0.  Sums are fp32 whatever the dtype.
+ *
+ * The backward pass takes the cotangent gy of y (dev [n_rows, H] in grad_dtype elements), the x, gamma, p and
+ * state of the forward call and its mean and rstd, and returns in fp32 dx [n_rows, H] (the gh of
+ * jitdb_treelstm_backward, if x is h), dgamma [H], dbeta [H], all overwritten.  n_rows == 0 zeroes dgamma and dbeta.
+ */
+int jitdb_layernorm_forward(const void *x, const float *gamma, const float *beta, int64_t n_rows, int32_t H,
+                            jitdb_dtype dtype, float eps, float p, const uint64_t *state,
+                            void *y, float *mean, float *rstd, void *hip_stream);
+size_t jitdb_layernorm_backward_workspace_bytes(int64_t n_rows, int32_t H, jitdb_dtype dtype);
+int jitdb_layernorm_backward(const void *x, const float *gamma, const float *mean, const float *rstd,
+                             const void *gy, int64_t n_rows, int32_t H, jitdb_dtype dtype, jitdb_dtype grad_dtype,
+                             float p, const uint64_t *state, float *dx, float *dgamma, float *dbeta,
+                             void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * Softmax cross entropy over classes or words, with its gradient.  The logits of the batch are never kept.
+ *     z_nc = <h_n, V_c> + b_c      lse_n = log sum_c exp(z_nc)      loss_n = lse_n - z_n,label(n)
+ *
+ *   h        dev [n_rows, H] in dtype elements
+ *   V        dev [n_classes, H] in dtype elements
+ *   b        dev [n_classes] fp32 or NULL (= zeros); -inf takes a class out
+ *   label    dev [n_rows] int32.  -1: the row has no label; it is not multiplied, its loss and lse are 0 and
+ *            its gradient is 0, whatever h holds there.  Any other value outside [0, n_classes): the row's loss,
+ *            and with it the gradients it has a part in, are NaN.
+ *   loss, lse  dev [n_rows] fp32, out
+ * 1 <= H <= 16384, 1 <= n_classes <= JITDB_MAX_CLASSES.
+ *
+ * The backward pass takes the lse of the forward call and the cotangent gloss of loss (dev [n_rows] fp32, or NULL:
+ * 1 for every row), and returns, all overwritten,
+ *     dh [n_rows, H], dV [n_classes, H] in grad_dtype elements, db [n_classes] in fp32.
+ * grad_dtype is JITDB_F32 (dh is then the gh of jitdb_treelstm_backward, if h is the forward's), or JITDB_BF16 for bf16
+ * operands: the derivatives of the logits are then bf16 operands of the two products, which takes about half the time.
+ * n_rows == 0 zeroes dV and db.
+ */
+#define JITDB_MAX_CLASSES (1 << 22)
+size_t jitdb_softmax_xent_workspace_bytes(int64_t n_rows, int32_t H, int32_t n_classes, jitdb_dtype dtype);
+int jitdb_softmax_xent_forward(const void *h, const void *V, const float *b, const int32_t *label,
+                               int64_t n_rows, int32_t H, int32_t n_classes, jitdb_dtype dtype,
+                               float *loss, float *lse,
+                               void *workspace, size_t workspace_bytes, void *hip_stream);
+size_t jitdb_softmax_xent_backward_workspace_bytes(int64_t n_rows, int32_t H, int32_t n_classes,
+                                                   jitdb_dtype dtype, jitdb_dtype grad_dtype);
+int jitdb_softmax_xent_backward(const void *h, const void *V, const float *b, const int32_t *label,
+                                const float *lse, const float *gloss,
+                                int64_t n_rows, int32_t H, int32_t n_classes, jitdb_dtype dtype,
+                                jitdb_dtype grad_dtype, void *dh, void *dV, float *db,
+                                void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
  * Per-kernel timing, for measuring the execution step against the hardware
  * roofline (the paper reports only wall-clock samples/s, section 5; the
  * kernels here are this implementation's own).  Between jitdb_profile_start
@@ -517,9 +596,10 @@ const char *jitdb_last_hip_error(void);
  * Library version, "major.minor".  The structs of this header are written by the library and carry no size, so a
  * program must be compiled against the header of the library it runs with: one whose JITDB_VERSION differs from
  * jitdb_version() must not call anything else.  0.2 added tree_window and tree_tag to jitdb_schedule_t and
- * JITDB_K_TREES to the arrays of jitdb_profile_t; both are longer than in 0.1.
+ * JITDB_K_TREES to the arrays of jitdb_profile_t; both are longer than in 0.1.  0.3 added the calls of a training step's
+ * head (layer norm, dropout, loss); its structs are those of 0.2.
  */
-#define JITDB_VERSION "0.2"
+#define JITDB_VERSION "0.3"
 const char *jitdb_version(void);
 
 #ifdef __cplusplus

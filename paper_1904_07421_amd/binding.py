@@ -17,7 +17,7 @@ import numpy as np
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libjitdb.so")
 
-_VERSION = "0.2"            # JITDB_VERSION of the header that the structs below follow
+_VERSION = "0.3"            # JITDB_VERSION of the header that the structs below follow
 
 JITDB_F32 = 0
 JITDB_CELL_CHILDSUM = 0
@@ -136,6 +136,25 @@ def load_library():
         ctypes.POINTER(_ScheduleStruct), ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p,
         ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p,
         ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]
+    vp, i32, i64, f32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float
+    lib.jitdb_dropout.restype = ctypes.c_int
+    lib.jitdb_dropout.argtypes = [vp, i64, ctypes.c_int, f32, vp, vp, vp]
+    lib.jitdb_layernorm_forward.restype = ctypes.c_int
+    lib.jitdb_layernorm_forward.argtypes = [vp, vp, vp, i64, i32, ctypes.c_int, f32, f32, vp, vp, vp, vp, vp]
+    lib.jitdb_layernorm_backward_workspace_bytes.restype = ctypes.c_size_t
+    lib.jitdb_layernorm_backward_workspace_bytes.argtypes = [i64, i32, ctypes.c_int]
+    lib.jitdb_layernorm_backward.restype = ctypes.c_int
+    lib.jitdb_layernorm_backward.argtypes = [vp, vp, vp, vp, vp, i64, i32, ctypes.c_int, ctypes.c_int, f32, vp, vp, vp, vp,
+                                             vp, ctypes.c_size_t, vp]
+    lib.jitdb_softmax_xent_workspace_bytes.restype = ctypes.c_size_t
+    lib.jitdb_softmax_xent_workspace_bytes.argtypes = [i64, i32, i32, ctypes.c_int]
+    lib.jitdb_softmax_xent_forward.restype = ctypes.c_int
+    lib.jitdb_softmax_xent_forward.argtypes = [vp, vp, vp, vp, i64, i32, i32, ctypes.c_int, vp, vp, vp, ctypes.c_size_t, vp]
+    lib.jitdb_softmax_xent_backward_workspace_bytes.restype = ctypes.c_size_t
+    lib.jitdb_softmax_xent_backward_workspace_bytes.argtypes = [i64, i32, i32, ctypes.c_int, ctypes.c_int]
+    lib.jitdb_softmax_xent_backward.restype = ctypes.c_int
+    lib.jitdb_softmax_xent_backward.argtypes = [vp, vp, vp, vp, vp, vp, i64, i32, i32, ctypes.c_int, ctypes.c_int, vp, vp, vp,
+                                                vp, ctypes.c_size_t, vp]
     lib.jitdb_profile_start.restype = ctypes.c_int
     lib.jitdb_profile_start.argtypes = [ctypes.c_int32]
     lib.jitdb_profile_stop.restype = ctypes.c_int
@@ -862,3 +881,189 @@ def jitdb_treelstm_forward_packed(x, packed: PackedWeights, schedule: Schedule, 
             workspace.data_ptr(), workspace.numel(), _stream_ptr(stream))
     _check(code)
     return h, c
+
+
+# ---- the head of a training step: layer norm, dropout, loss ------------------------------------------------
+def _dtype_of(t, name):
+    import torch
+    if t.dtype == torch.float32:
+        return JITDB_F32
+    if t.dtype == torch.bfloat16:
+        return JITDB_BF16
+    raise TypeError(f"{name} must be float32 or bfloat16")
+
+
+def _dense(device, *tensors):
+    """(tensor, name, dtype, shape) each: contiguous, on `device`; tensors that are None are skipped."""
+    for t, name, dtype, shape in tensors:
+        if t is None:
+            continue
+        if not t.is_cuda or not t.is_contiguous() or t.dtype != dtype:
+            raise TypeError(f"{name} must be a contiguous {str(dtype).replace('torch.', '')} CUDA tensor")
+        if t.device != device:
+            raise ValueError(f"{name} lies on {t.device}, not on {device}")
+        if shape is not None and tuple(t.shape) != tuple(shape):
+            raise ValueError(f"{name} must be {list(shape)}, not {list(t.shape)}")
+
+
+def _head_workspace(stream, workspace, need, device):
+    import torch
+    if workspace is None:
+        return _empty(stream, max(need, 256), dtype=torch.uint8, device=device)
+    _dense(device, (workspace, "workspace", torch.uint8, None))
+    return workspace
+
+
+def _ptr(t):
+    return t.data_ptr() if t is not None and t.numel() else None
+
+
+def _drop_state(p, state, device):
+    import torch
+    if not 0.0 <= p <= 1.0:
+        raise ValueError("p must lie in [0, 1]")
+    if state is None:
+        if p > 0.0:
+            raise ValueError("dropout needs state, an int64 CUDA tensor of two values: seed, first word")
+        return
+    _dense(device, (state, "state", torch.int64, (2,)))
+
+
+def jitdb_dropout(x, p: float, state, stream=None, out=None):
+    """x (float32 or bfloat16 CUDA tensor of any shape) with its elements kept with probability 1 - p and scaled by
+    1 / (1 - p), the others 0.  state: int64 CUDA tensor [2] = (seed, first word of the generator's stream); the call uses
+    (x.numel() + 1) // 2 words.  The same call on the cotangent of the result gives that of x.  out may be x."""
+    import torch
+    dt = _dtype_of(x, "x")
+    _dense(x.device, (x, "x", x.dtype, None), (out, "out", x.dtype, x.shape))
+    if state is None:
+        raise ValueError("dropout needs state, an int64 CUDA tensor of two values: seed, first word")
+    _drop_state(p, state, x.device)
+    y = _empty(stream, x.shape, dtype=x.dtype, device=x.device) if out is None else out
+    with _on_device(x.device):
+        _check(load_library().jitdb_dropout(_ptr(x), x.numel(), dt, p, state.data_ptr(), _ptr(y), _stream_ptr(stream)))
+    return y
+
+
+def jitdb_layernorm_forward(x, gamma, beta, eps: float = 1e-5, p: float = 0.0, state=None, stream=None,
+                            out: Optional[Tuple] = None):
+    """Layer norm of the rows of x [N, H] (float32 or bfloat16), gamma, beta [H] fp32, with dropout behind it if p > 0
+    (state as in jitdb_dropout).  Returns (y [N, H] in x's dtype, mean [N] fp32, rstd [N] fp32); `out` = those three reuses
+    buffers (y may be x)."""
+    import torch
+    dt = _dtype_of(x, "x")
+    if x.dim() != 2:
+        raise ValueError("x must be [N, H]")
+    n, H = x.shape
+    f32 = torch.float32
+    _dense(x.device, (x, "x", x.dtype, None), (gamma, "gamma", f32, (H,)), (beta, "beta", f32, (H,)))
+    _drop_state(p, state, x.device)
+    if out is None:
+        y = _empty(stream, (n, H), dtype=x.dtype, device=x.device)
+        mean, rstd = _empty(stream, n, dtype=f32, device=x.device), _empty(stream, n, dtype=f32, device=x.device)
+    else:
+        y, mean, rstd = out
+        _dense(x.device, (y, "y", x.dtype, (n, H)), (mean, "mean", f32, (n,)), (rstd, "rstd", f32, (n,)))
+    with _on_device(x.device):
+        _check(load_library().jitdb_layernorm_forward(_ptr(x), _ptr(gamma), _ptr(beta), n, H, dt, eps, p, _ptr(state), _ptr(y),
+                                                      _ptr(mean), _ptr(rstd), _stream_ptr(stream)))
+    return y, mean, rstd
+
+
+def jitdb_layernorm_backward_workspace_bytes(n_rows: int, H: int, dtype: int) -> int:
+    return int(load_library().jitdb_layernorm_backward_workspace_bytes(int(n_rows), int(H), int(dtype)))
+
+
+def jitdb_layernorm_backward(x, gamma, mean, rstd, gy, p: float = 0.0, state=None, stream=None, workspace=None,
+                             out: Optional[Tuple] = None):
+    """From the cotangent gy [N, H] (float32 or bfloat16) of jitdb_layernorm_forward's y and that call's x, gamma, mean, rstd,
+    p and state: fp32 (dx [N, H], dgamma [H], dbeta [H])."""
+    import torch
+    dt, gdt = _dtype_of(x, "x"), _dtype_of(gy, "gy")
+    if x.dim() != 2:
+        raise ValueError("x must be [N, H]")
+    n, H = x.shape
+    f32 = torch.float32
+    _dense(x.device, (x, "x", x.dtype, None), (gamma, "gamma", f32, (H,)), (mean, "mean", f32, (n,)), (rstd, "rstd", f32, (n,)),
+           (gy, "gy", gy.dtype, (n, H)))
+    _drop_state(p, state, x.device)
+    if out is None:
+        dx = _empty(stream, (n, H), dtype=f32, device=x.device)
+        dgamma, dbeta = _empty(stream, H, dtype=f32, device=x.device), _empty(stream, H, dtype=f32, device=x.device)
+    else:
+        dx, dgamma, dbeta = out
+        _dense(x.device, (dx, "dx", f32, (n, H)), (dgamma, "dgamma", f32, (H,)), (dbeta, "dbeta", f32, (H,)))
+    workspace = _head_workspace(stream, workspace, jitdb_layernorm_backward_workspace_bytes(n, H, dt), x.device)
+    with _on_device(x.device):
+        _check(load_library().jitdb_layernorm_backward(
+            _ptr(x), _ptr(gamma), _ptr(mean), _ptr(rstd), _ptr(gy), n, H, dt, gdt, p, _ptr(state), _ptr(dx), _ptr(dgamma),
+            _ptr(dbeta), workspace.data_ptr(), workspace.numel(), _stream_ptr(stream)))
+    return dx, dgamma, dbeta
+
+
+def _xent_shapes(h, V, label, b):
+    import torch
+    dt = _dtype_of(h, "h")
+    if h.dim() != 2 or V.dim() != 2:
+        raise ValueError("h must be [N, H] and V [C, H]")
+    n, H = h.shape
+    C = V.shape[0]
+    _dense(h.device, (h, "h", h.dtype, None), (V, "V", h.dtype, (C, H)), (label, "label", torch.int32, (n,)),
+           (b, "b", torch.float32, (C,)))
+    return dt, n, H, C
+
+
+def jitdb_softmax_xent_workspace_bytes(n_rows: int, H: int, n_classes: int, dtype: int) -> int:
+    return int(load_library().jitdb_softmax_xent_workspace_bytes(int(n_rows), int(H), int(n_classes), int(dtype)))
+
+
+def jitdb_softmax_xent_forward(h, V, label, b=None, stream=None, workspace=None, out: Optional[Tuple] = None):
+    """Softmax cross entropy of the rows of h [N, H] under class weights V [C, H] (both float32 or both bfloat16), bias b [C]
+    fp32 or None, label [N] int32 (-1: no label).  Returns fp32 (loss [N], lse [N]), 0 for rows without a label."""
+    import torch
+    dt, n, H, C = _xent_shapes(h, V, label, b)
+    if out is None:
+        loss, lse = (_empty(stream, n, dtype=torch.float32, device=h.device) for _ in range(2))
+    else:
+        loss, lse = out
+        _dense(h.device, (loss, "loss", torch.float32, (n,)), (lse, "lse", torch.float32, (n,)))
+    workspace = _head_workspace(stream, workspace, jitdb_softmax_xent_workspace_bytes(n, H, C, dt), h.device)
+    with _on_device(h.device):
+        _check(load_library().jitdb_softmax_xent_forward(
+            _ptr(h), _ptr(V), _ptr(b), _ptr(label), n, H, C, dt, _ptr(loss), _ptr(lse), workspace.data_ptr(),
+            workspace.numel(), _stream_ptr(stream)))
+    return loss, lse
+
+
+def jitdb_softmax_xent_backward_workspace_bytes(n_rows: int, H: int, n_classes: int, dtype: int, grad_dtype: int) -> int:
+    return int(load_library().jitdb_softmax_xent_backward_workspace_bytes(int(n_rows), int(H), int(n_classes), int(dtype),
+                                                                          int(grad_dtype)))
+
+
+def jitdb_softmax_xent_backward(h, V, label, lse, gloss=None, b=None, grad_dtype=None, stream=None, workspace=None,
+                                out: Optional[Tuple] = None):
+    """Gradients of sum <gloss, loss> (gloss [N] fp32, or None = ones) from what jitdb_softmax_xent_forward was given and its
+    lse: (dh [N, H], dV [C, H] in grad_dtype, db [C] fp32).  grad_dtype: torch.float32 (the default; dh is then the gh of
+    jitdb_treelstm_backward), or torch.bfloat16 for bfloat16 operands, which is faster."""
+    import torch
+    dt, n, H, C = _xent_shapes(h, V, label, b)
+    f32 = torch.float32
+    if grad_dtype is None:
+        grad_dtype = f32
+    if grad_dtype not in (f32, h.dtype):
+        raise TypeError("grad_dtype must be float32, or bfloat16 for bfloat16 operands")
+    _dense(h.device, (lse, "lse", f32, (n,)), (gloss, "gloss", f32, (n,)))
+    gdt = JITDB_F32 if grad_dtype == f32 else JITDB_BF16
+    if out is None:
+        dh = _empty(stream, (n, H), dtype=grad_dtype, device=h.device)
+        dV = _empty(stream, (C, H), dtype=grad_dtype, device=h.device)
+        db = _empty(stream, C, dtype=f32, device=h.device)
+    else:
+        dh, dV, db = out
+        _dense(h.device, (dh, "dh", grad_dtype, (n, H)), (dV, "dV", grad_dtype, (C, H)), (db, "db", f32, (C,)))
+    workspace = _head_workspace(stream, workspace, jitdb_softmax_xent_backward_workspace_bytes(n, H, C, dt, gdt), h.device)
+    with _on_device(h.device):
+        _check(load_library().jitdb_softmax_xent_backward(
+            _ptr(h), _ptr(V), _ptr(b), _ptr(label), _ptr(lse), _ptr(gloss), n, H, C, dt, gdt, _ptr(dh), _ptr(dV), _ptr(db),
+            workspace.data_ptr(), workspace.numel(), _stream_ptr(stream)))
+    return dh, dV, db

@@ -16,15 +16,7 @@ namespace jitdb {
 namespace {
 
 constexpr int kT = 1024;
-constexpr uint64_t kGolden = 0x9E3779B97F4A7C15ull;
 constexpr uint64_t kKey1 = 0xD1B54A32D192ED03ull;
-
-// output function of SplitMix64
-__device__ __forceinline__ uint64_t mix64(uint64_t z) {
-    z = (z ^ (z >> 30)) * 0xBF58476D1CE4E5B9ull;
-    z = (z ^ (z >> 27)) * 0x94D049BB133111EBull;
-    return z ^ (z >> 31);
-}
 
 __global__ void __launch_bounds__(64)
 fingerprint_clear_kernel(unsigned long long *fp) {

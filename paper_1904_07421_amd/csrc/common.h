@@ -88,6 +88,14 @@ template <typename T> __device__ __forceinline__ float to_f32(T v);
 template <> __device__ __forceinline__ float to_f32<float>(float v) { return v; }
 template <> __device__ __forceinline__ float to_f32<bf16_t>(bf16_t v) { return bf16_to_f32(v); }
 
+// ---- SplitMix64: its increment and its output function (fingerprints of forests, dropout)
+constexpr uint64_t kGolden = 0x9E3779B97F4A7C15ull;
+__device__ __forceinline__ uint64_t mix64(uint64_t z) {
+    z = (z ^ (z >> 30)) * 0xBF58476D1CE4E5B9ull;
+    z = (z ^ (z >> 27)) * 0x94D049BB133111EBull;
+    return z ^ (z >> 31);
+}
+
 // K-blocked operand layout of the tiled GEMM core: bytes [64 s, 64 s + 64) of every row form
 // slab s, rows consecutive inside a slab (n_rows_alloc rows per slab).  Byte offset of byte
 // `kbyte` of row `row`.
