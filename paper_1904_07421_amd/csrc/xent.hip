@@ -1,5 +1,5 @@
 // Softmax cross entropy over classes or words: loss of every labelled node and the gradients of states, class weights and bias,
-// without the logits of the batch ever being kept.
+// without the logits of the batch ever being kept.  (Few classes take the kernels of xent_few.h.)
 //
 //     z_nc = <h_n, V_c> + b_c     lse_n = log sum_c exp z_nc     loss_n = lse_n - z_n,label(n)
 //     g_nc = gloss_n (exp(z_nc - lse_n) - [c = label(n)])
@@ -17,7 +17,7 @@
 // is itself rounded to 2^-8), in three parts where they leave in fp32 (two would leave 2.5e-6 of them, as a norm: more than the fp32
 // sums do).  The bias' gradient sums fp32 values.
 
-#include "level_common.h"
+#include "xent_few.h"
 
 namespace jitdb {
 namespace {
@@ -870,6 +870,39 @@ int run_backward_xent(const T *h, const T *V, const float *b, const RowList &lis
     return JITDB_OK;
 }
 
+// ---- few classes ---------------------------------------------------------------------------------------
+// Is there a variant for these sizes?
+bool few_fits(int H, int C, jitdb_dtype dtype) {
+    auto any = [](auto, auto) {};
+    return dtype == JITDB_F32 ? for_few<float>(H, C, any) : for_few<bf16_t>(H, C, any);
+}
+int few_blocks(int64_t n) {              // of the backward pass: each leaves a set of sums
+    const int64_t b = ceil_div(n, kFewRows);
+    return (int)(b < 1024 ? b : 1024);
+}
+size_t few_part_bytes(int64_t n, int H, int C) {
+    Carver c(nullptr);
+    c.take<float>((size_t)few_blocks(n > 0 ? n : 1) * ((size_t)C * H + C));
+    return c.off;
+}
+template <typename T>
+int run_few_forward(const FewArgs &a, hipStream_t st) {
+    const int64_t b = ceil_div(a.n, kFewRows);
+    const unsigned blocks = (unsigned)(b < 2048 ? b : 2048);
+    for_few<T>(a.H, a.C, [&](auto c, auto nb) { few_forward_kernel<T, decltype(c)::value, decltype(nb)::value><<<blocks, kFewT, 0, st>>>(a); });
+    JITDB_LAUNCH_CHECK();
+    return JITDB_OK;
+}
+template <typename T, typename O>
+int run_few_backward(const FewArgs &a, O *dV, float *db, hipStream_t st) {
+    const int blocks = few_blocks(a.n);
+    for_few<T>(a.H, a.C, [&](auto c, auto nb) { few_backward_kernel<T, O, decltype(c)::value, decltype(nb)::value><<<blocks, kFewT, 0, st>>>(a); });
+    JITDB_LAUNCH_CHECK();
+    few_reduce_kernel<O><<<(unsigned)ceil_div((int64_t)a.C * a.H + a.C, 64), 1024, 0, st>>>(a.part, blocks, a.H, a.C, dV, db);
+    JITDB_LAUNCH_CHECK();
+    return JITDB_OK;
+}
+
 bool off_type(const void *p, jitdb_dtype t) { return reinterpret_cast<uintptr_t>(p) & (t == JITDB_F32 ? 3 : 1); }
 bool off_word(const void *p) { return reinterpret_cast<uintptr_t>(p) & 3; }
 
@@ -880,12 +913,14 @@ using namespace jitdb;
 
 extern "C" size_t jitdb_softmax_xent_workspace_bytes(int64_t n_rows, int32_t H, int32_t n_classes, jitdb_dtype dtype) {
     Sizes s;
-    return make_sizes(n_rows, H, n_classes, dtype, dtype, s) ? carve(s, false, nullptr).bytes : 0;
+    if (!make_sizes(n_rows, H, n_classes, dtype, dtype, s)) return 0;
+    return few_fits(H, n_classes, dtype) ? 256 : carve(s, false, nullptr).bytes;      // (few classes need none: never 0, which is an error)
 }
 extern "C" size_t jitdb_softmax_xent_backward_workspace_bytes(int64_t n_rows, int32_t H, int32_t n_classes, jitdb_dtype dtype,
                                                               jitdb_dtype grad_dtype) {
     Sizes s;
-    return make_sizes(n_rows, H, n_classes, dtype, grad_dtype, s) ? carve(s, true, nullptr).bytes : 0;
+    if (!make_sizes(n_rows, H, n_classes, dtype, grad_dtype, s)) return 0;
+    return few_fits(H, n_classes, dtype) ? few_part_bytes(n_rows, H, n_classes) : carve(s, true, nullptr).bytes;
 }
 
 extern "C" int jitdb_softmax_xent_forward(const void *h, const void *V, const float *b, const int32_t *label,
@@ -899,8 +934,13 @@ extern "C" int jitdb_softmax_xent_forward(const void *h, const void *V, const fl
     if (off_type(h, dtype) || off_type(V, dtype) || off_word(b) || off_word(label) || off_word(loss) || off_word(lse) ||
         (reinterpret_cast<uintptr_t>(workspace) & 255))
         return JITDB_E_BADARG;
+    if (workspace_bytes < jitdb_softmax_xent_workspace_bytes(n_rows, H, n_classes, dtype)) return JITDB_E_WORKSPACE;
+    if (few_fits(H, n_classes, dtype)) {
+        FewArgs a = {};
+        a.h = h; a.V = V; a.b = b; a.label = label; a.n = n_rows; a.H = H; a.C = n_classes; a.loss = loss; a.lse = lse;
+        return dtype == JITDB_F32 ? run_few_forward<float>(a, (hipStream_t)hip_stream) : run_few_forward<bf16_t>(a, (hipStream_t)hip_stream);
+    }
     const Space w = carve(s, false, workspace);
-    if (workspace_bytes < w.bytes) return JITDB_E_WORKSPACE;
     RowList list = {};
     list.label = label; list.n = n_rows; list.C = n_classes; list.counts = w.counts; list.n_rows = w.n_rows;
     list.row_of = w.row_of; list.label_of = w.label_of; list.loss_out = loss; list.lse_out = lse;
@@ -933,8 +973,16 @@ extern "C" int jitdb_softmax_xent_backward(const void *h, const void *V, const f
     if (off_type(h, dtype) || off_type(V, dtype) || off_word(b) || off_word(label) || off_word(lse) || off_word(gloss) ||
         off_type(dh, grad_dtype) || (reinterpret_cast<uintptr_t>(workspace) & 255))
         return JITDB_E_BADARG;
+    if (workspace_bytes < jitdb_softmax_xent_backward_workspace_bytes(n_rows, H, n_classes, dtype, grad_dtype)) return JITDB_E_WORKSPACE;
+    if (few_fits(H, n_classes, dtype)) {
+        FewArgs a = {};
+        a.h = h; a.V = V; a.b = b; a.label = label; a.n = n_rows; a.H = H; a.C = n_classes; a.lse_in = lse; a.gloss = gloss;
+        a.dh = dh; a.part = static_cast<float *>(workspace);
+        if (dtype == JITDB_F32) return run_few_backward<float, float>(a, static_cast<float *>(dV), db, st);
+        if (grad_dtype == JITDB_F32) return run_few_backward<bf16_t, float>(a, static_cast<float *>(dV), db, st);
+        return run_few_backward<bf16_t, bf16_t>(a, static_cast<bf16_t *>(dV), db, st);
+    }
     const Space w = carve(s, true, workspace);
-    if (workspace_bytes < w.bytes) return JITDB_E_WORKSPACE;
     RowList list = {};
     list.label = label; list.lse = lse; list.gloss = gloss; list.n = n_rows; list.C = n_classes; list.counts = w.counts;
     list.n_rows = w.n_rows; list.row_of = w.row_of; list.label_of = w.label_of; list.lse_of = w.lse_of; list.w_of = w.w_of;

@@ -1,0 +1,337 @@
+// Softmax cross entropy over few classes (up to 64): bound by memory, so every state is read once from HBM and everything that
+// is computed from it happens while it passes.
+//
+// The class weights lie in LDS.  A wave works on 16 rows: their logits come from fp32 matrix instructions (16 classes x 16 rows, K = 4;
+// a lane holds one row and four classes of every 16), so that statistics are sums over four lanes' registers; the derivatives g of the
+// logits are in the place where the product g V wants them, and the rows' gradients leave at once.  The weights' gradients sum over
+// rows: the 64 rows of a block put their g into LDS, and each wave adds them to its own quarter of the features, reading the
+// states a second time out of L2, now with a feature in each lane.  Blocks keep their sums in registers to the end;
+// few_reduce_kernel adds the blocks in order.
+#pragma once
+
+#include "level_common.h"
+
+namespace jitdb {
+namespace {
+
+constexpr int kFewT = 256;               // threads of a block: four waves
+constexpr int kFewRows = 64;             // rows a block works on at once
+template <typename T> constexpr int kFewVec = 16 / (int)sizeof(T);        // elements of one load
+template <typename T> constexpr int kFewBlock = 64 * kFewVec<T>;          // features that four waves cover with one load a lane
+
+struct FewArgs {
+    const void *h, *V;
+    const float *b;
+    const int32_t *label;
+    int64_t n;
+    int H, C;
+    // forward
+    float *loss, *lse;
+    // backward
+    const float *lse_in, *gloss;
+    void *dh;
+    float *part;                         // [blocks][C H + C]
+};
+
+// The weights in LDS: in the order of the logits' loads, K in steps of four loads side by side.  Element e of piece (step s, quarter q)
+// of class i; 17 pieces instead of 16 spread the other reader, who wants one element of 4 x 16 pieces at once, over the banks.
+template <typename T>
+__device__ __forceinline__ int few_at(int steps, int ct, int s, int q, int i, int e) {
+    return ((((ct * steps + s) * 4 + q) * 17) + i) * kFewVec<T> + e;
+}
+template <typename T, int CT, int NB>
+struct FewTable {
+    static constexpr int kSteps = NB * kFewBlock<T> / (4 * kFewVec<T>);
+    T w[CT * kSteps * 4 * 17 * kFewVec<T>];
+    float bias[CT * 16];
+    __device__ __forceinline__ void load(const FewArgs &a) {
+        constexpr int V = kFewVec<T>;
+        const T *src = static_cast<const T *>(a.V);
+        const int steps = (a.H + 4 * V - 1) / (4 * V) + 1;      // the gradient goes by 32 features: at most one more step
+        for (int p = threadIdx.x; p < CT * 16 * steps * 4; p += kFewT) {
+            const int piece = p % (steps * 4), c = p / (steps * 4), s = piece >> 2, q = piece & 3, k = piece * V;
+            if (s >= kSteps) continue;
+            T e[V];
+#pragma unroll
+            for (int j = 0; j < V; ++j) e[j] = c < a.C && k + j < a.H ? src[(int64_t)c * a.H + k + j] : T(0);
+            __builtin_memcpy(&w[few_at<T>(kSteps, c >> 4, s, q, c & 15, 0)], e, 16);
+        }
+        for (int c = threadIdx.x; c < CT * 16; c += kFewT) bias[c] = c >= a.C ? -INFINITY : a.b ? a.b[c] : 0.0f;
+    }
+};
+
+template <typename T, int N>
+__device__ __forceinline__ void few_load(const T *p, int left, float (&v)[N]) {
+    T e[N];
+    if (left >= N) {
+        __builtin_memcpy(e, p, sizeof(e));
+    } else {
+#pragma unroll
+        for (int k = 0; k < N; ++k) e[k] = k < left ? p[k] : T(0);
+    }
+#pragma unroll
+    for (int k = 0; k < N; ++k) v[k] = to_f32<T>(e[k]);
+}
+
+// z[ct][v]: logit of class 16 ct + 4 (lane / 16) + v, row `row` (that of the lane; every sixteenth lane has the same), bias and all
+template <typename T, int CT, int NB>
+__device__ __forceinline__ void few_logits(const FewArgs &a, const FewTable<T, CT, NB> &t, const T *row, bool has, floatx4 (&z)[CT]) {
+    constexpr int V = kFewVec<T>, STEPS = FewTable<T, CT, NB>::kSteps;
+    const int lane = threadIdx.x & 63, i = lane & 15, q = lane >> 4;
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) z[ct][v] = t.bias[ct * 16 + q * 4 + v];
+    auto step = [&](int s, const float (&x)[V]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) {
+            T e[V];
+            __builtin_memcpy(e, &t.w[few_at<T>(STEPS, ct, s, q, i, 0)], 16);
+#pragma unroll
+            for (int j = 0; j < V; ++j) z[ct] = __builtin_amdgcn_mfma_f32_16x16x4f32(to_f32<T>(e[j]), x[j], z[ct], 0, 0, 0);
+        }
+    };
+    const int whole = a.H / (4 * V);
+    int s = 0;
+    for (; s + 4 <= whole; s += 4) {                 // four loads in flight
+        float x[4][V];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) few_load<T, V>(row + (s + u) * 4 * V + q * V, has ? V : 0, x[u]);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) step(s + u, x[u]);
+    }
+    for (; s * 4 * V < a.H; ++s) {
+        float x[V];
+        const int k = s * 4 * V + q * V;
+        few_load<T, V>(row + k, has ? a.H - k : 0, x);
+        step(s, x);
+    }
+}
+__device__ __forceinline__ float quarters_max(float v) {
+    v = fmaxf(v, __shfl_xor(v, 16));
+    return fmaxf(v, __shfl_xor(v, 32));
+}
+__device__ __forceinline__ float quarters_sum(float v) {
+    v += __shfl_xor(v, 16);
+    return v + __shfl_xor(v, 32);
+}
+
+template <typename T, int CT, int NB>
+__global__ void __launch_bounds__(kFewT)
+few_forward_kernel(const FewArgs a) {
+    __shared__ FewTable<T, CT, NB> table;
+    table.load(a);
+    __syncthreads();
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, q = lane >> 4;
+    const T *h = static_cast<const T *>(a.h);
+    for (int64_t r0 = ((int64_t)blockIdx.x * 4 + wave) * 16; r0 < a.n; r0 += (int64_t)gridDim.x * kFewRows) {
+        const int64_t r = r0 + (lane & 15);
+        const int label = r < a.n ? a.label[r] : -1;
+        const bool has = label != -1;
+        float loss = 0.0f, lse = 0.0f;
+        if (__any(has)) {
+            floatx4 z[CT];
+            few_logits<T, CT, NB>(a, table, h + (has ? r : 0) * a.H, has, z);
+            float top = -INFINITY, at = 0.0f, s = 0.0f;
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+                for (int v = 0; v < 4; ++v) {
+                    top = fmaxf(top, z[ct][v]);
+                    if (label == ct * 16 + q * 4 + v) at = z[ct][v];
+                }
+            top = quarters_max(top);
+            const float from = top == -INFINITY ? 0.0f : top;       // every class masked: the sum is 0, not NaN
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+                for (int v = 0; v < 4; ++v) s += expf(z[ct][v] - from);
+            lse = from + logf(quarters_sum(s));
+            at = quarters_sum(at);
+            loss = label >= 0 && label < a.C ? lse - at : __builtin_nanf("");
+        }
+        if (q == 0 && r < a.n) {
+            a.loss[r] = has ? loss : 0.0f;
+            a.lse[r] = has ? lse : 0.0f;
+        }
+    }
+}
+
+template <typename T, typename O, int CT, int NB>
+__global__ void __launch_bounds__(kFewT)
+few_backward_kernel(const FewArgs a) {
+    constexpr int V = kFewVec<T>, STEPS = FewTable<T, CT, NB>::kSteps, COLS = CT * 16;
+    __shared__ FewTable<T, CT, NB> table;
+    __shared__ __attribute__((aligned(16))) float gs[2][kFewRows][COLS];
+    __shared__ int32_t has_of[2][kFewRows];
+    table.load(a);
+    __syncthreads();
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i16 = lane & 15, q = lane >> 4, H = a.H;
+    const T *h = static_cast<const T *>(a.h);
+    O *dh = static_cast<O *>(a.dh);
+    floatx4 dv[NB][V][CT];                           // feature (nb 4 + wave) 16 V + i16 V + e, classes 16 ct + 4 q + v
+    float db[CT][4];
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+            db[ct][v] = 0.0f;
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                for (int e = 0; e < V; ++e) dv[nb][e][ct][v] = 0.0f;
+        }
+    int turn = 0;
+    for (int64_t b0 = (int64_t)blockIdx.x * kFewRows; b0 < a.n; b0 += (int64_t)gridDim.x * kFewRows, turn ^= 1) {
+        const int64_t r = b0 + wave * 16 + i16;
+        const int label = r < a.n ? a.label[r] : -1;
+        const bool has = label != -1;
+        floatx4 g[CT];
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) g[ct] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+        if (__any(has)) {
+            floatx4 z[CT];
+            few_logits<T, CT, NB>(a, table, h + (has ? r : 0) * H, has, z);
+            const float lse = has ? a.lse_in[r] : 0.0f;
+            const float w = !has ? 0.0f : label < 0 || label >= a.C ? __builtin_nanf("") : a.gloss ? a.gloss[r] : 1.0f;
+            if (has)
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) {
+                        const int c = ct * 16 + q * 4 + v;
+                        // classes past the last have p = 0 and weights of 0: they add nothing, also in rows that are NaN
+                        const float d = expf(z[ct][v] - lse) - (label == c ? 1.0f : 0.0f);
+                        g[ct][v] = c < a.C ? d * w : 0.0f;
+                        db[ct][v] += g[ct][v];
+                    }
+        }
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) *reinterpret_cast<floatx4 *>(&gs[turn][wave * 16 + i16][ct * 16 + q * 4]) = g[ct];
+        if (q == 0) has_of[turn][wave * 16 + i16] = has;
+        // dh of the wave's rows, 32 features at a time: a lane has eight of its row's, 8 q .. 8 q + 7
+        for (int f0 = 0; f0 < H; f0 += 32) {
+            floatx4 d[2] = {{0.0f, 0.0f, 0.0f, 0.0f}, {0.0f, 0.0f, 0.0f, 0.0f}};
+            const int fi = f0 + (i16 >> 2) * 8 + (i16 & 3);          // the feature whose weights this lane brings, + 4 for the second product
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const int f = fi + 4 * u, s = f / (4 * V), fq = f / V & 3, e = f % V;
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+                    for (int v = 0; v < 4; ++v)
+                        d[u] = __builtin_amdgcn_mfma_f32_16x16x4f32(to_f32<T>(table.w[few_at<T>(STEPS, ct, s, fq, q * 4 + v, e)]), g[ct][v], d[u], 0, 0, 0);
+            }
+            if (r < a.n) {
+                O e[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) e[k] = from_f32<O>(has ? d[k >> 2][k & 3] : 0.0f);
+                const int f = f0 + q * 8;
+                O *o = dh + r * H + f;
+                if (f + 8 <= H) {
+                    __builtin_memcpy(o, e, sizeof(e));
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        if (f + k < H) o[k] = e[k];
+                }
+            }
+        }
+        __syncthreads();                             // the 64 rows' g is there; the other buffer is free again behind the next one
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+            const int f = ((nb * 4 + wave) * 16 + i16) * V;
+            if ((nb * 4 + wave) * 16 * V >= H) continue;
+            for (int k0 = 0; k0 < kFewRows; k0 += 16) {
+                float x[4][V];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int rr = k0 + 4 * k + q;
+                    const bool on = has_of[turn][rr];
+                    few_load<T, V>(h + (on ? (b0 + rr) * H + f : 0), on ? H - f : 0, x[k]);
+                }
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+#pragma unroll
+                    for (int ct = 0; ct < CT; ++ct) {
+                        const float ga = gs[turn][k0 + 4 * k + q][ct * 16 + i16];
+#pragma unroll
+                        for (int e = 0; e < V; ++e) dv[nb][e][ct] = __builtin_amdgcn_mfma_f32_16x16x4f32(ga, x[k][e], dv[nb][e][ct], 0, 0, 0);
+                    }
+            }
+        }
+    }
+    float *part = a.part + (int64_t)blockIdx.x * ((int64_t)a.C * H + a.C);
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+                const int c = ct * 16 + q * 4 + v, f = ((nb * 4 + wave) * 16 + i16) * V;
+                if (c < a.C)
+#pragma unroll
+                    for (int e = 0; e < V; ++e)
+                        if (f + e < H) part[(int64_t)c * H + f + e] = dv[nb][e][ct][v];
+            }
+    // the bias: over the 16 lanes that hold the same classes, then the four waves
+    __syncthreads();
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+            float s = db[ct][v];
+#pragma unroll
+            for (int m = 1; m < 16; m <<= 1) s += __shfl_xor(s, m);
+            if (i16 == 0) gs[0][wave][ct * 16 + q * 4 + v] = s;
+        }
+    __syncthreads();
+    if ((int)threadIdx.x < a.C)
+        part[(int64_t)a.C * H + threadIdx.x] = gs[0][0][threadIdx.x] + gs[0][1][threadIdx.x] + gs[0][2][threadIdx.x] + gs[0][3][threadIdx.x];
+}
+
+// Value c of [n_parts][C H + C]: 64 values a block, sixteen waves take every sixteenth part in order, then the sixteen in order.
+template <typename O>
+__global__ void __launch_bounds__(1024)
+few_reduce_kernel(const float *__restrict__ part, int n_parts, int H, int C, O *__restrict__ dV, float *__restrict__ db) {
+    __shared__ float sums[16][64];
+    const int64_t weights = (int64_t)C * H, width = weights + C;
+    const int l = threadIdx.x & 63, q = threadIdx.x >> 6;
+    const int64_t c = (int64_t)blockIdx.x * 64 + l;
+    float s = 0.0f;
+    if (c < width)
+#pragma unroll 8
+        for (int p = q; p < n_parts; p += 16) s += part[p * width + c];
+    sums[q][l] = s;
+    __syncthreads();
+    if (q || c >= width) return;
+    for (int k = 1; k < 16; ++k) s += sums[k][l];
+    if (c < weights) dV[c] = from_f32<O>(s);
+    else db[c - weights] = s;
+}
+
+// The variant of H features and C classes: launch(classes / 16, blocks of features), false where the weights do not fit LDS with the rest.
+template <typename T, typename F>
+bool for_few(int H, int C, F &&launch) {
+    const int nb = (int)ceil_div(H, kFewBlock<T>), ct = (int)ceil_div(C, 16);
+    auto with = [&](auto c, auto b) {
+        constexpr int CT = decltype(c)::value, NB = decltype(b)::value;
+        // 128 registers of sums a lane; weights and two sets of g in LDS
+        if constexpr (CT * NB * kFewVec<T> <= 32 && sizeof(FewTable<T, CT, NB>) + 2 * kFewRows * (CT * 64 + 4) <= 160 * 1024) { launch(c, b); return true; }
+        return false;
+    };
+    auto blocks = [&](auto c) {
+        if (nb <= 1) return with(c, std::integral_constant<int, 1>());
+        if (nb <= 2) return with(c, std::integral_constant<int, 2>());
+        if (nb <= 4) return with(c, std::integral_constant<int, 4>());
+        if (nb <= 8) return with(c, std::integral_constant<int, 8>());
+        return false;
+    };
+    if (ct <= 1) return blocks(std::integral_constant<int, 1>());
+    if (ct <= 2) return blocks(std::integral_constant<int, 2>());
+    if (ct <= 4) return blocks(std::integral_constant<int, 4>());
+    return false;
+}
+
+}  // namespace
+}  // namespace jitdb
