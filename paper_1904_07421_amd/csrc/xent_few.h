@@ -1,9 +1,9 @@
 // Softmax cross entropy over few classes (up to 64): bound by memory, so every state is read once from HBM and everything that
 // is computed from it happens while it passes.
 //
-// The class weights lie in LDS.  A wave works on 16 rows: their logits come from fp32 matrix instructions (16 classes x 16 rows, K = 4;
-// a lane holds one row and four classes of every 16), so that statistics are sums over four lanes' registers; the derivatives g of the
-// logits are in the place where the product g V wants them, and the rows' gradients leave at once.  The weights' gradients sum over
+// The class weights lie in LDS.  A wave works on 16 rows: their logits come from the matrix instructions of 16 classes x 16 rows (a
+// lane holds one row and four classes of every 16), so that statistics are sums over four lanes' registers; the derivatives g of the
+// logits are in the place where the product g V (fp32 matrix instructions, as for the weights' gradients) wants them, and the rows' gradients leave at once.  The weights' gradients sum over
 // rows: the 64 rows of a block put their g into LDS, and each wave adds them to its own quarter of the features, reading the
 // states a second time out of L2, now with a feature in each lane.  Blocks keep their sums in registers to the end;
 // few_reduce_kernel adds the blocks in order.
@@ -60,17 +60,25 @@ struct FewTable {
     }
 };
 
-template <typename T, int N>
-__device__ __forceinline__ void few_load(const T *p, int left, float (&v)[N]) {
-    T e[N];
-    if (left >= N) {
-        __builtin_memcpy(e, p, sizeof(e));
-    } else {
+// Sixteen bytes of a row as they are; only the first `left` elements exist (none: zeros).
+template <typename T>
+__device__ __forceinline__ u32x4 few_load(const T *p, int left) {
+    constexpr int V = kFewVec<T>;
+    u32x4 w = {0u, 0u, 0u, 0u};
+    if (left >= V) {
+        __builtin_memcpy(&w, p, 16);
+    } else if (left > 0) {
+        T e[V];
 #pragma unroll
-        for (int k = 0; k < N; ++k) e[k] = k < left ? p[k] : T(0);
+        for (int k = 0; k < V; ++k) e[k] = k < left ? p[k] : T(0);
+        __builtin_memcpy(&w, e, 16);
     }
-#pragma unroll
-    for (int k = 0; k < N; ++k) v[k] = to_f32<T>(e[k]);
+    return w;
+}
+template <typename T>
+__device__ __forceinline__ float few_element(const u32x4 &w, int e) {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(w[e]);
+    else return __uint_as_float(e & 1 ? w[e >> 1] & 0xFFFF0000u : w[e >> 1] << 16);
 }
 
 // z[ct][v]: logit of class 16 ct + 4 (lane / 16) + v, row `row` (that of the lane; every sixteenth lane has the same), bias and all
@@ -82,30 +90,25 @@ __device__ __forceinline__ void few_logits(const FewArgs &a, const FewTable<T, C
     for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
         for (int v = 0; v < 4; ++v) z[ct][v] = t.bias[ct * 16 + q * 4 + v];
-    auto step = [&](int s, const float (&x)[V]) __attribute__((always_inline)) {
+    auto step = [&](int s, const u32x4 &x) __attribute__((always_inline)) {
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) {
-            T e[V];
-            __builtin_memcpy(e, &t.w[few_at<T>(STEPS, ct, s, q, i, 0)], 16);
-#pragma unroll
-            for (int j = 0; j < V; ++j) z[ct] = __builtin_amdgcn_mfma_f32_16x16x4f32(to_f32<T>(e[j]), x[j], z[ct], 0, 0, 0);
+            u32x4 w;
+            __builtin_memcpy(&w, &t.w[few_at<T>(STEPS, ct, s, q, i, 0)], 16);
+            mfma16<T>(w, x, z[ct]);                  // (products of bf16 values are exact)
         }
     };
-    const int whole = a.H / (4 * V);
+    const int whole = has ? a.H / (4 * V) : 0, steps = (a.H + 4 * V - 1) / (4 * V);
+    const T *at = row + q * V;
     int s = 0;
-    for (; s + 4 <= whole; s += 4) {                 // four loads in flight
-        float x[4][V];
+    for (; s + 4 <= a.H / (4 * V); s += 4) {         // four loads in flight
+        u32x4 x[4];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) few_load<T, V>(row + (s + u) * 4 * V + q * V, has ? V : 0, x[u]);
+        for (int u = 0; u < 4; ++u) x[u] = few_load<T>(at + (s + u) * 4 * V, whole ? V : 0);
 #pragma unroll
         for (int u = 0; u < 4; ++u) step(s + u, x[u]);
     }
-    for (; s * 4 * V < a.H; ++s) {
-        float x[V];
-        const int k = s * 4 * V + q * V;
-        few_load<T, V>(row + k, has ? a.H - k : 0, x);
-        step(s, x);
-    }
+    for (; s < steps; ++s) step(s, few_load<T>(at + s * 4 * V, has ? a.H - (s * 4 + q) * V : 0));
 }
 __device__ __forceinline__ float quarters_max(float v) {
     v = fmaxf(v, __shfl_xor(v, 16));
@@ -158,7 +161,7 @@ few_forward_kernel(const FewArgs a) {
 }
 
 template <typename T, typename O, int CT, int NB>
-__global__ void __launch_bounds__(kFewT)
+__global__ void __launch_bounds__(kFewT, CT * NB * kFewVec<T> <= 8 ? 4 : 1)
 few_backward_kernel(const FewArgs a) {
     constexpr int V = kFewVec<T>, STEPS = FewTable<T, CT, NB>::kSteps, COLS = CT * 16;
     __shared__ FewTable<T, CT, NB> table;
@@ -242,23 +245,29 @@ few_backward_kernel(const FewArgs a) {
         for (int nb = 0; nb < NB; ++nb) {
             const int f = ((nb * 4 + wave) * 16 + i16) * V;
             if ((nb * 4 + wave) * 16 * V >= H) continue;
-            for (int k0 = 0; k0 < kFewRows; k0 += 16) {
-                float x[4][V];
+            // four rows a quarter in flight; `left`: elements of the lane's piece (a block of features that ends inside one is the exception)
+            auto add = [&](int left) __attribute__((always_inline)) {
+                for (int k0 = 0; k0 < kFewRows; k0 += 16) {
+                    u32x4 x[4];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const int rr = k0 + 4 * k + q;
-                    const bool on = has_of[turn][rr];
-                    few_load<T, V>(h + (on ? (b0 + rr) * H + f : 0), on ? H - f : 0, x[k]);
-                }
-#pragma unroll
-                for (int k = 0; k < 4; ++k)
-#pragma unroll
-                    for (int ct = 0; ct < CT; ++ct) {
-                        const float ga = gs[turn][k0 + 4 * k + q][ct * 16 + i16];
-#pragma unroll
-                        for (int e = 0; e < V; ++e) dv[nb][e][ct] = __builtin_amdgcn_mfma_f32_16x16x4f32(ga, x[k][e], dv[nb][e][ct], 0, 0, 0);
+                    for (int k = 0; k < 4; ++k) {
+                        const int rr = k0 + 4 * k + q;
+                        const bool on = has_of[turn][rr];
+                        x[k] = few_load<T>(h + (on ? (b0 + rr) * H + f : 0), on ? left : 0);
                     }
-            }
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+#pragma unroll
+                        for (int ct = 0; ct < CT; ++ct) {
+                            const float ga = gs[turn][k0 + 4 * k + q][ct * 16 + i16];
+#pragma unroll
+                            for (int e = 0; e < V; ++e)
+                                dv[nb][e][ct] = __builtin_amdgcn_mfma_f32_16x16x4f32(ga, few_element<T>(x[k], e), dv[nb][e][ct], 0, 0, 0);
+                        }
+                }
+            };
+            if (((nb * 4 + wave) * 16 + 16) * V <= H) add(V);
+            else add(H - f);
         }
     }
     float *part = a.part + (int64_t)blockIdx.x * ((int64_t)a.C * H + a.C);
