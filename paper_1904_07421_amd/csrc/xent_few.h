@@ -212,13 +212,15 @@ few_backward_kernel(const FewArgs a) {
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) *reinterpret_cast<floatx4 *>(&gs[turn][wave * 16 + i16][ct * 16 + q * 4]) = g[ct];
         if (q == 0) has_of[turn][wave * 16 + i16] = has;
-        // dh of the wave's rows, 32 features at a time: a lane has eight of its row's, 8 q .. 8 q + 7
+        // dh of the wave's rows, 32 features at a time in two products: a lane has four of its row's in each, so placed that it
+        // stores sixteen bytes (fp32: 4 q .. 4 q + 3 of either half; bf16: 8 q .. 8 q + 7).  Nothing reads dh soon: past the caches,
+        // where the states wait for their second reading
         for (int f0 = 0; f0 < H; f0 += 32) {
             floatx4 d[2] = {{0.0f, 0.0f, 0.0f, 0.0f}, {0.0f, 0.0f, 0.0f, 0.0f}};
-            const int fi = f0 + (i16 >> 2) * 8 + (i16 & 3);          // the feature whose weights this lane brings, + 4 for the second product
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-                const int f = fi + 4 * u, s = f / (4 * V), fq = f / V & 3, e = f % V;
+                const int f = f0 + (sizeof(O) == 4 ? u * 16 + i16 : (i16 >> 2) * 8 + u * 4 + (i16 & 3));    // whose weights this lane brings
+                const int s = f / (4 * V), fq = f / V & 3, e = f % V;
 #pragma unroll
                 for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
@@ -226,17 +228,24 @@ few_backward_kernel(const FewArgs a) {
                         d[u] = __builtin_amdgcn_mfma_f32_16x16x4f32(to_f32<T>(table.w[few_at<T>(STEPS, ct, s, fq, q * 4 + v, e)]), g[ct][v], d[u], 0, 0, 0);
             }
             if (r < a.n) {
+                constexpr int PER = 16 / (int)sizeof(O);
                 O e[8];
 #pragma unroll
                 for (int k = 0; k < 8; ++k) e[k] = from_f32<O>(has ? d[k >> 2][k & 3] : 0.0f);
-                const int f = f0 + q * 8;
-                O *o = dh + r * H + f;
-                if (f + 8 <= H) {
-                    __builtin_memcpy(o, e, sizeof(e));
-                } else {
 #pragma unroll
-                    for (int k = 0; k < 8; ++k)
-                        if (f + k < H) o[k] = e[k];
+                for (int u = 0; u < 8 / PER; ++u) {
+                    const int f = f0 + u * 16 + q * PER;
+                    O *o = dh + r * H + f;
+                    if (f + PER <= H) {
+                        typedef u32x4 __attribute__((aligned(2))) any4;
+                        u32x4 w;
+                        __builtin_memcpy(&w, e + u * PER, 16);
+                        __builtin_nontemporal_store(w, reinterpret_cast<any4 *>(o));
+                    } else {
+#pragma unroll
+                        for (int k = 0; k < PER; ++k)
+                            if (f + k < H) o[k] = e[u * PER + k];
+                    }
                 }
             }
         }
