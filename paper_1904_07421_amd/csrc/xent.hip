@@ -18,6 +18,7 @@
 // sums do).  The bias' gradient sums fp32 values.
 
 #include "xent_few.h"
+#include "xent_resident.h"
 
 namespace jitdb {
 namespace {
@@ -533,14 +534,21 @@ label_logit_kernel(const T *__restrict__ h, const T *__restrict__ V, const float
     }
 }
 
-// 64 rows a block; wave w takes every fourth tile's statistics, then the four are put together
+// 64 rows a block; wave w takes every fourth set of statistics, then the four are put together.  The sets are `n_stat` of max_rows
+// rows, or, class_tiles > 0, those that resident_logits_kernel left.
 __global__ void __launch_bounds__(kT)
-join_kernel(const float2 *__restrict__ stat, int n_stat, int row0, int max_rows, const int32_t *__restrict__ n_rows,
+join_kernel(const float2 *__restrict__ stat, int n_stat, int class_tiles, int row0, int max_rows, const int32_t *__restrict__ n_rows,
             const int32_t *__restrict__ row_of, const float *__restrict__ label_z, float *__restrict__ loss, float *__restrict__ lse) {
     __shared__ float2 red[4][64];
     const int rows = chunk_rows(n_rows, row0, max_rows);
     if ((int)blockIdx.x * 64 >= rows) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = blockIdx.x * 64 + lane;
+    int64_t stride = max_rows;
+    if (class_tiles > 0) {
+        const int blocks = (rows + kResRows - 1) / kResRows;
+        n_stat = res_splits(blocks, class_tiles, kResPlaces);
+        stride = (int64_t)blocks * kResRows;
+    }
     float top = -INFINITY, s = 0.0f;
     auto add = [&](float2 p) {
         if (p.y == 0.0f) return;                     // nothing but masked classes
@@ -550,7 +558,7 @@ join_kernel(const float2 *__restrict__ stat, int n_stat, int row0, int max_rows,
     };
     if (r < rows)
 #pragma unroll 4
-        for (int k = wave; k < n_stat; k += 4) add(stat[(int64_t)k * max_rows + r]);
+        for (int k = wave; k < n_stat; k += 4) add(stat[k * stride + r]);
     red[wave][lane] = make_float2(top, s);
     __syncthreads();
     if (wave || r >= rows) return;
@@ -669,12 +677,12 @@ grad_finish_kernel(const GradArgs a) {
         }
     }
 }
-// 64 classes a block; sixteen waves take every sixteenth row tile, in order
+// 64 classes a block; sixteen waves take every sixteenth of the sums that `per` of each 256 rows left, in order
 __global__ void __launch_bounds__(1024)
-bias_grad_kernel(const float *__restrict__ part, int n_classes_pad, int C, const int32_t *__restrict__ n_rows, int row0, int max_rows,
+bias_grad_kernel(const float *__restrict__ part, int n_classes_pad, int per, int C, const int32_t *__restrict__ n_rows, int row0, int max_rows,
                  int first, float *__restrict__ db) {
     __shared__ float sums[16][64];
-    const int tiles = (chunk_rows(n_rows, row0, max_rows) + kTileB - 1) / kTileB;
+    const int tiles = (chunk_rows(n_rows, row0, max_rows) + kTileB - 1) / kTileB * per;
     const int l = threadIdx.x & 63, q = threadIdx.x >> 6, c = blockIdx.x * 64 + l;
     float s = 0.0f;
     if (c < C)
@@ -707,15 +715,23 @@ struct Sizes {
     int H, C, Hk, Hf, Cp;      // widths: of K (states), of the turned weights' rows, classes in whole tiles
     int parts, g_parts;        // of the operands, of g
     int label_blocks;
+    int res, class_tiles;      // resident_logits_kernel: K in steps of 16 (0: not for this width), tiles of 32 classes (an even number)
     int stat_rows, grad_rows;  // rows of a chunk
 };
 bool known(jitdb_dtype t) { return t == JITDB_F32 || t == JITDB_BF16; }
+// K in steps of 16 of the variant of resident_logits_kernel for this width: the states of 64 rows in up to 256 registers
+int res_steps(int H, jitdb_dtype dtype) {
+    if (dtype == JITDB_F32) return H <= 64 ? 4 : H <= 128 ? 8 : H <= 160 ? 10 : 0;
+    return H <= 128 ? 8 : H <= 256 ? 16 : H <= 384 ? 24 : H <= 512 ? 32 : 0;
+}
 bool make_sizes(int64_t n, int32_t H, int32_t C, jitdb_dtype dtype, jitdb_dtype grad, Sizes &s) {
     if (n < 0 || n > JITDB_MAX_NODES || H < 1 || H > kMaxWidth || C < 1 || C > kMaxClasses || !known(dtype) || !known(grad)) return false;
     if (dtype == JITDB_F32 && grad == JITDB_BF16) return false;       // gradients are not rounded below their operands
     s.n = n; s.H = H; s.C = C;
     s.n_pad = round_up(n > 0 ? n : 1, kTileB);
-    s.Hk = (int)round_up(H, 64);
+    s.res = res_steps(H, dtype);
+    s.class_tiles = (int)round_up(C, 64) / kResClasses;
+    s.Hk = s.res ? s.res * 16 : (int)round_up(H, 64);
     s.Hf = (int)round_up(H, kTileA);
     s.Cp = (int)round_up(C, kTileA);
     s.parts = dtype == JITDB_F32 ? 3 : 1;
@@ -725,7 +741,7 @@ bool make_sizes(int64_t n, int32_t H, int32_t C, jitdb_dtype dtype, jitdb_dtype 
         const int64_t rows = budget / bytes_a_row / kTileB * kTileB;
         return (int)(rows < kTileB ? kTileB : rows < s.n_pad ? rows : s.n_pad);
     };
-    s.stat_rows = chunk((int64_t)s.Cp / 64 * 8, kStatBytes);
+    s.stat_rows = s.res ? (int)s.n_pad : chunk((int64_t)s.Cp / 64 * 8, kStatBytes);
     s.grad_rows = chunk((int64_t)s.Cp * 2 * s.g_parts, kGradBytes);
     return true;
 }
@@ -734,6 +750,12 @@ int64_t grad_parts(int64_t tiles, int64_t stages) {
     const int64_t ranges = stages / kMinStages > 1 ? stages / kMinStages : 1;
     const int64_t filled = tiles * ranges < kSlots ? tiles * ranges : kSlots;
     return tiles > filled ? tiles : filled;
+}
+// most blocks of resident_logits_kernel, whatever the rows (res_splits)
+int64_t res_blocks(int64_t rows, int class_tiles) {
+    const int64_t rb = ceil_div(rows, kResRows), ranges = class_tiles / kResMinTiles > 1 ? class_tiles / kResMinTiles : 1;
+    const int64_t most = rb > kResBlocks ? rb : kResBlocks;
+    return rb * ranges < most ? rb * ranges : most;
 }
 struct Space {
     int32_t *counts, *n_rows, *row_of, *label_of;
@@ -756,18 +778,18 @@ Space carve(const Sizes &s, bool backward, void *base) {
     w.n_rows = c.take<int32_t>(1);
     w.row_of = c.take<int32_t>(s.n_pad);
     w.label_of = c.take<int32_t>(s.n_pad);
-    w.bias = c.take<float>(s.Cp);
+    w.bias = c.take<float>(s.Cp + 64);
     w.h = take_operand(c, s.parts, s.Hk / 32, s.n_pad);
     w.v = take_operand(c, s.parts, s.Hk / 32, s.Cp);
     if (!backward) {
         w.label_z = c.take<float>(s.n_pad);
-        w.stat = c.take<float2>((size_t)(s.Cp / 64) * s.stat_rows);
+        w.stat = c.take<float2>(s.res ? (size_t)res_blocks(s.n_pad, s.class_tiles) * kResRows : (size_t)(s.Cp / 64) * s.stat_rows);
     } else {
         w.lse_of = c.take<float>(s.n_pad);
         w.w_of = c.take<float>(s.n_pad);
         w.vt = take_operand(c, s.parts, s.Cp / 32, s.Hf);
         w.g = take_operand(c, s.g_parts, s.Cp / 32, s.grad_rows);
-        w.db_part = c.take<float>((size_t)(s.grad_rows / kTileB) * s.Cp);
+        w.db_part = c.take<float>((size_t)(s.grad_rows / kTileB) * (s.res ? 4 : 1) * s.Cp);
         w.part_h = c.take<float>((size_t)(grad_parts((int64_t)s.Hf / kTileA * (s.grad_rows / kTileB), s.Cp / 32) * kTileA * kTileB));
         w.part_v = c.take<float>((size_t)(grad_parts((int64_t)s.Cp / kTileA * ceil_div(s.H, kTileB), s.grad_rows / 32) * kTileA * kTileB));
         if (s.grad_rows < s.n) w.acc_v = c.take<float>((size_t)s.C * s.H);
@@ -793,7 +815,7 @@ int prepare(const T *h, const T *V, const float *b, const RowList &list, const S
     JITDB_LAUNCH_CHECK();
     pack_rows_kernel<T, PARTS><<<grid_of((int64_t)s.Cp * (s.Hk / 8)), kT, 0, st>>>(V, nullptr, nullptr, s.C, s.H, s.Hk / 32, kTileA, w.v);
     JITDB_LAUNCH_CHECK();
-    pad_bias_kernel<<<grid_of(s.Cp), kT, 0, st>>>(b, s.C, s.Cp, w.bias);
+    pad_bias_kernel<<<grid_of(s.Cp + 64), kT, 0, st>>>(b, s.C, s.Cp + 64, w.bias);
     JITDB_LAUNCH_CHECK();
     return JITDB_OK;
 }
@@ -805,6 +827,31 @@ LogitArgs logit_args(const Sizes &s, const Space &w) {
     return a;
 }
 
+ResArgs res_args(const Sizes &s, const Space &w) {
+    ResArgs a = {};
+    a.V = w.v.at; a.v_slab = w.v.slab; a.h = w.h.at; a.h_slab = w.h.slab;
+    a.bias = w.bias; a.class_tiles = s.class_tiles; a.n_rows = w.n_rows;
+    a.label_of = w.label_of; a.lse_of = w.lse_of; a.w_of = w.w_of;
+    a.g = w.g.at; a.g_slab = w.g.slab; a.g_part = w.g.part; a.db_part = w.db_part;
+    return a;
+}
+template <typename T, int G>
+int launch_resident(int steps, int64_t rows, const ResArgs &a, hipStream_t st) {
+    const unsigned grid = tile_grid(res_blocks(rows, a.class_tiles));
+    if constexpr (sizeof(T) == 4) {
+        if (steps == 4) resident_logits_kernel<3, 4, G><<<grid, kResT, 0, st>>>(a);
+        else if (steps == 8) resident_logits_kernel<3, 8, G><<<grid, kResT, 0, st>>>(a);
+        else resident_logits_kernel<3, 10, G><<<grid, kResT, 0, st>>>(a);
+    } else {
+        if (steps == 8) resident_logits_kernel<1, 8, G><<<grid, kResT, 0, st>>>(a);
+        else if (steps == 16) resident_logits_kernel<1, 16, G><<<grid, kResT, 0, st>>>(a);
+        else if (steps == 24) resident_logits_kernel<1, 24, G><<<grid, kResT, 0, st>>>(a);
+        else resident_logits_kernel<1, 32, G><<<grid, kResT, 0, st>>>(a);
+    }
+    JITDB_LAUNCH_CHECK();
+    return JITDB_OK;
+}
+
 template <typename T>
 int run_forward_xent(const T *h, const T *V, const float *b, const RowList &list, const Sizes &s, const Space &w,
                      float *loss, float *lse, hipStream_t st) {
@@ -813,6 +860,15 @@ int run_forward_xent(const T *h, const T *V, const float *b, const RowList &list
     const int64_t label_blocks = ceil_div(s.n, 4);
     label_logit_kernel<T><<<(unsigned)(label_blocks < 8192 ? label_blocks : 8192), kT, 0, st>>>(h, V, b, w.n_rows, w.row_of, w.label_of, s.H, w.label_z);
     JITDB_LAUNCH_CHECK();
+    if (s.res) {
+        ResArgs a = res_args(s, w);
+        a.stat = w.stat;
+        a.max_rows = (int)s.n_pad;
+        if ((rc = launch_resident<T, 0>(s.res, s.n, a, st)) != JITDB_OK) return rc;
+        join_kernel<<<(unsigned)ceil_div(s.n, 64), kT, 0, st>>>(w.stat, 0, s.class_tiles, 0, a.max_rows, w.n_rows, w.row_of, w.label_z, loss, lse);
+        JITDB_LAUNCH_CHECK();
+        return JITDB_OK;
+    }
     LogitArgs a = logit_args(s, w);
     a.stat = w.stat;
     a.max_rows = s.stat_rows;
@@ -821,7 +877,7 @@ int run_forward_xent(const T *h, const T *V, const float *b, const RowList &list
         const int64_t rows = s.n - r0 < s.stat_rows ? s.n - r0 : s.stat_rows;
         logits_kernel<0, sizeof(T) == 4><<<tile_grid(ceil_div(rows, kTileB) * a.n_class_tiles), kT, 0, st>>>(a);
         JITDB_LAUNCH_CHECK();
-        join_kernel<<<(unsigned)ceil_div(rows, 64), kT, 0, st>>>(w.stat, 2 * a.n_class_tiles, a.row0, a.max_rows, w.n_rows, w.row_of, w.label_z, loss, lse);
+        join_kernel<<<(unsigned)ceil_div(rows, 64), kT, 0, st>>>(w.stat, 2 * a.n_class_tiles, 0, a.row0, a.max_rows, w.n_rows, w.row_of, w.label_z, loss, lse);
         JITDB_LAUNCH_CHECK();
     }
     return JITDB_OK;
@@ -841,20 +897,28 @@ int run_backward_xent(const T *h, const T *V, const float *b, const RowList &lis
     LogitArgs a = logit_args(s, w);
     a.label_of = w.label_of; a.lse_of = w.lse_of; a.w_of = w.w_of; a.g = w.g; a.db_part = w.db_part;
     a.max_rows = s.grad_rows;
+    ResArgs ra = res_args(s, w);
+    ra.max_rows = s.grad_rows;
     GradArgs gh = {}, gv = {};
     gh.p.A = w.vt; gh.p.B = w.g; gh.p.pairs = make_pairs(w.vt, s.parts, w.g, s.g_parts);
-    gh.a_tiles = s.Hf / kTileA; gh.class_stages = s.Cp / 32; gh.part = w.part_h; gh.out = dh; gh.row_of = w.row_of;
+    gh.a_tiles = s.Hf / kTileA; gh.class_stages = s.class_tiles; gh.part = w.part_h; gh.out = dh; gh.row_of = w.row_of;
     gv.p.A = w.g; gv.p.B = w.h; gv.p.pairs = make_pairs(w.g, s.g_parts, w.h, s.parts);
-    gv.a_tiles = s.Cp / kTileA; gv.a_slabs = s.Cp / 32; gv.b_slabs = s.Hk / 32;
+    gv.a_tiles = s.Cp / kTileA; gv.a_slabs = s.class_tiles; gv.b_slabs = s.Hk / 32;
     gv.tiles_most = gv.a_tiles * (int)ceil_div(s.H, kTileB); gv.part = w.part_v; gv.out = dV; gv.acc = w.acc_v;
     for (GradArgs *g : {&gh, &gv}) { g->n_rows = w.n_rows; g->max_rows = s.grad_rows; g->H = s.H; g->C = s.C; }
     for (int64_t r0 = 0; r0 < s.n; r0 += s.grad_rows) {
         const int64_t rows = s.n - r0 < s.grad_rows ? s.n - r0 : s.grad_rows, row_tiles = ceil_div(rows, kTileB);
         a.row0 = gh.row0 = gv.row0 = (int)r0;
         gv.first = r0 == 0; gv.last = r0 + s.grad_rows >= s.n;
-        logits_kernel<G_PARTS, sizeof(T) == 4><<<tile_grid(row_tiles * a.n_class_tiles), kT, 0, st>>>(a);
-        JITDB_LAUNCH_CHECK();
-        bias_grad_kernel<<<(unsigned)ceil_div(s.C, 64), 1024, 0, st>>>(w.db_part, s.Cp, s.C, w.n_rows, a.row0, a.max_rows, gv.first, db);
+        if (s.res) {
+            ra.row0 = (int)r0;
+            ra.h = w.h.at + r0 * 64;
+            if ((rc = launch_resident<T, G_PARTS>(s.res, rows, ra, st)) != JITDB_OK) return rc;
+        } else {
+            logits_kernel<G_PARTS, sizeof(T) == 4><<<tile_grid(row_tiles * a.n_class_tiles), kT, 0, st>>>(a);
+            JITDB_LAUNCH_CHECK();
+        }
+        bias_grad_kernel<<<(unsigned)ceil_div(s.C, 64), 1024, 0, st>>>(w.db_part, s.res ? s.class_tiles * kResClasses : s.Cp, s.res ? 4 : 1, s.C, w.n_rows, a.row0, a.max_rows, gv.first, db);
         JITDB_LAUNCH_CHECK();
         const int64_t h_tiles = gh.a_tiles * row_tiles;
         gv.p.B.at = w.h.at + r0 * 64;
