@@ -1,0 +1,415 @@
+// C = A^T B or A B^T in tiles, both operands streaming through LDS: the gradients' products, and logits of wide states.
+//
+// 2 WM waves multiply a tile of 64 WM rows of A (128 or 256) and 256 rows of B; each 2 x 4 MFMA tiles of 32 x 32.  In a 32 x 32 tile
+// lane l holds row l % 32 of B and rows 8 q + 4 (l / 32) + e of A (q, e < 4).  K runs over stages of 64 bytes a row (32 bf16) that travel
+// straight into LDS, one barrier a stage.  K_ROWS: the reduction runs over the operands' rows instead (32 a stage; a tile takes slabs of 32
+// columns each), transposed on the way out of LDS.  Two waves share a SIMD: eight of a block with WM = 4, of two blocks with WM = 2 (for
+// operands of at most 128 rows).  (Four waves of twice the size, alone on their SIMDs, read less LDS and were no faster.)
+// A direct load writes the 64 lanes' pieces to 1024 consecutive LDS bytes, 16 rows of 64: piece p of row r is kept in slot
+// p ^ ((r >> 2) & 3), so that a fragment read of 16 rows touches 16 distinct 16-byte columns.
+#pragma once
+
+#include "xent_resident.h"
+
+namespace jitdb {
+namespace {
+
+constexpr int kTileB = 256;                           // rows of B in a tile
+constexpr int kMaxPairs = 6;
+template <int WM> constexpr int kTileA = 64 * WM;     // rows of A
+template <int WM> constexpr int kTileT = 128 * WM;    // threads
+template <int WM> constexpr int kTileBufs = WM == 4 ? 4 : 3;
+template <int WM> constexpr int kTileBuf = (kTileA<WM> + kTileB) * 64;
+template <int WM> constexpr int kTilePlaces = WM == 4 ? 256 : 512;      // blocks the chip holds at once
+
+// Operands are K-blocked as in operand_offset, in one to three bf16 parts: part p, slab s (32 elements of K), row r
+// at + p * part + s * slab + r * 64.
+struct Operand {
+    char *at;
+    int64_t slab, part;
+};
+// The part products of one product, smallest first: where the parts lie behind each operand's first.  (Whole words: the
+// compiler reads them with scalar loads, which the K loop's hand-counted waits for vector memory do not see.)
+struct Pairs {
+    int64_t a[kMaxPairs], b[kMaxPairs];
+    int n;
+};
+inline Pairs make_pairs(const Operand &a, int parts_a, const Operand &b, int parts_b) {
+    Pairs p = {};
+    for (int w = 2; w >= 0; --w)
+        for (int i = 0; i <= w; ++i)
+            if (i < parts_a && w - i < parts_b) { p.a[p.n] = i * a.part; p.b[p.n] = (w - i) * b.part; ++p.n; }
+    return p;
+}
+struct Product {
+    Operand A, B;
+    Pairs pairs;
+    int a_slabs, b_slabs;           // K_ROWS: slabs there are; what lies behind the last is never read
+};
+
+// acc += stages s0 .. s0 + n_stages (n_stages >= 1) of the `nk` stages of each part product, one product behind the other; a0, b0: the
+// tile's first row of each operand (K_ROWS: first slab)
+template <bool K_ROWS, int WM>
+__device__ __forceinline__ void multiply_tile(const Product &p, int64_t a0, int64_t b0, int nk, int s0, int n_stages, char *lds, floatx16 (&acc)[2][4]) {
+    constexpr int A_UNITS = 4 * WM, LOADS = (A_UNITS + 16) / (2 * WM), BUFS = kTileBufs<WM>, BUF = kTileBuf<WM>, B_AT = A_UNITS * 1024;
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave >> 1, wn = wave & 1, hf = lane >> 5, l32 = lane & 31, lrow = lane >> 2;
+    // movers: 1 KB units of 16 rows of a slab, those of A in front of those of B, LOADS a wave
+    const char *from[LOADS];
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+        const int u = wave * LOADS + i, v = u < A_UNITS ? u : u - A_UNITS;
+        const Operand &o = u < A_UNITS ? p.A : p.B;
+        const int64_t first = u < A_UNITS ? a0 : b0;
+        if constexpr (K_ROWS) {
+            const int n_slabs = u < A_UNITS ? p.a_slabs : p.b_slabs;
+            const int64_t s = first + (v >> 1) < n_slabs ? first + (v >> 1) : n_slabs - 1;
+            from[i] = o.at + s * o.slab + ((v & 1) * 16 + lrow) * 64 + (lane & 3) * 16;
+        } else {
+            from[i] = o.at + (first + v * 16 + lrow) * 64 + ((lane & 3) ^ ((lane >> 4) & 3)) * 16;
+        }
+    }
+    const int64_t a_stage = K_ROWS ? 32 * 64 : p.A.slab, b_stage = K_ROWS ? 32 * 64 : p.B.slab;
+    int q = s0 / nk, k = s0 - q * nk, issued = 0;
+    int64_t a_off = p.pairs.a[q] + k * a_stage, b_off = p.pairs.b[q] + k * b_stage;
+    auto issue_one = [&](int buf, int i) __attribute__((always_inline)) {
+        const int u = wave * LOADS + i;
+        __builtin_amdgcn_global_load_lds(JITDB_GLOBAL_PTR(from[i] + (u < A_UNITS ? a_off : b_off)), JITDB_LDS_PTR(lds + buf * BUF + u * 1024), 16, 0, 0);
+    };
+    auto advance = [&]() __attribute__((always_inline)) {        // behind the last stage the last one is asked for again: the waits count on it
+        if (++issued >= n_stages) return;
+        a_off += a_stage;
+        b_off += b_stage;
+        if (++k == nk) {
+            k = 0;
+            ++q;
+            a_off = p.pairs.a[q];
+            b_off = p.pairs.b[q];
+        }
+    };
+    int a_rd[2], b_rd[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        if constexpr (K_ROWS) {
+            const int at = h * 1024 + (hf * 4 + ((lane & 15) >> 2)) * 64 + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
+            a_rd[h] = wm * 4096 + at;
+            b_rd[h] = B_AT + wn * 8192 + at;
+        } else {
+            const int slot16 = ((2 * h + hf) ^ ((l32 >> 2) & 3)) * 16;
+            a_rd[h] = (wm * 64 + l32) * 64 + slot16;
+            b_rd[h] = B_AT + (wn * 128 + l32) * 64 + slot16;
+        }
+    }
+    const uint32_t lds_base = (uint32_t)(uintptr_t)JITDB_LDS_PTR(lds);
+    struct Frags {
+        u32x4 a[2], b[4];
+    };
+    // tiles of 32 rows lie 2048 bytes apart in either layout
+    auto read_one = [&](auto tile, uint32_t at, u32x4 &f) __attribute__((always_inline)) {
+        constexpr int I = decltype(tile)::value;
+        if constexpr (K_ROWS) {
+            u32x2 lo, hi;
+            lds_read8_turned<I * 2048>(lo, at);
+            lds_read8_turned<I * 2048 + 512>(hi, at);
+            f = __builtin_shufflevector(lo, hi, 0, 1, 2, 3);
+        } else {
+            lds_read16<I * 2048>(f, at);
+        }
+    };
+    auto read_group = [&](int buf, int h, Frags &f) __attribute__((always_inline)) {
+        const uint32_t aa = lds_base + buf * BUF + a_rd[h], bb = lds_base + buf * BUF + b_rd[h];
+        static_for<4>([&](auto i) __attribute__((always_inline)) {
+            if constexpr (decltype(i)::value < 2) read_one(i, aa, f.a[decltype(i)::value]);
+            read_one(i, bb, f.b[decltype(i)::value]);
+        });
+    };
+    auto reads_done = [&](Frags &f) __attribute__((always_inline)) {
+        asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(f.a[0]), "+v"(f.a[1]), "+v"(f.b[0]), "+v"(f.b[1]), "+v"(f.b[2]), "+v"(f.b[3]));
+    };
+    auto multiply = [&](const Frags &f) __attribute__((always_inline)) {
+#pragma unroll
+        for (int m = 0; m < 8; ++m) mfma_step<bf16_t>(f.a[m / 4], f.b[m % 4], acc[m / 4][m % 4]);
+    };
+    // the next requests are dealt out between the MFMAs: a burst of them would hold the wave back until the memory pipeline took them
+    auto multiply_and_issue = [&](const Frags &f, int buf) __attribute__((always_inline)) {
+#pragma unroll
+        for (int m = 0; m < 8; ++m) {
+            mfma_step<bf16_t>(f.a[m / 4], f.b[m % 4], acc[m / 4][m % 4]);
+            __builtin_amdgcn_sched_barrier(0);
+            if (m < LOADS) issue_one(buf, m);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        advance();
+    };
+    auto wait_barrier = [&](auto n) __attribute__((always_inline)) {
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(decltype(n)::value) : "memory");
+    };
+    const std::integral_constant<int, (BUFS - 1) * LOADS> first_left;    // loads of younger stages that may stay in flight
+    const std::integral_constant<int, (BUFS - 2) * LOADS> next_left;
+    const std::integral_constant<int, 0> none_left;
+#pragma unroll
+    for (int b = 0; b < BUFS; ++b) {
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) issue_one(b, i);
+        advance();
+    }
+    Frags P, Q;
+    int cur = 0;
+    wait_barrier(first_left);
+    read_group(0, 0, P);
+    reads_done(P);
+    // P holds the first half of stage g (buffer cur), whose buffer is free for stage g + BUFS behind the barrier
+    for (int g = 0; g < n_stages; ++g) {
+        const int next = cur == BUFS - 1 ? 0 : cur + 1;
+        read_group(cur, 1, Q);
+        __builtin_amdgcn_sched_barrier(0);
+        multiply(P);
+        __builtin_amdgcn_sched_barrier(0);
+        reads_done(Q);
+        wait_barrier(next_left);
+        read_group(next, 0, P);
+        __builtin_amdgcn_sched_barrier(0);
+        multiply_and_issue(Q, cur);
+        __builtin_amdgcn_sched_barrier(0);
+        reads_done(P);
+        cur = next;
+    }
+    wait_barrier(none_left);             // nothing is on its way into the buffers, and every wave is done with them
+}
+
+__device__ __forceinline__ void clear_tile(floatx16 (&acc)[2][4]) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) acc[i][g][v] = 0.0f;
+}
+
+// Blocks are dealt round-robin to the 8 XCDs, each with an L2 of its own: XCD x takes the x-th eighth of the places in order.
+__device__ __forceinline__ int64_t xcd_order(int64_t total) {
+    const int64_t per = (total + 7) / 8, i = (int64_t)(blockIdx.x & 7) * per + (blockIdx.x >> 3);
+    return (blockIdx.x >> 3) < per && i < total ? i : -1;
+}
+__device__ __forceinline__ int chunk_rows(const int32_t *n_rows, int row0, int max_rows) {
+    const int left = *n_rows - row0;
+    return left < 0 ? 0 : left < max_rows ? left : max_rows;
+}
+
+// ---- the two products with g -------------------------------------------------------------------------
+// dh^T = V^T g^T: A = class weights, B = g, K = classes: the rows of both.  dV^T = h^T g: A = turned states, B = g, K = rows.  A's
+// rows (columns) are features in either, so that a lane ends with four features of a row or class side by side.
+// The stages of all tiles of B together are cut into equal ranges, as many as fill the chip, whatever the number of rows turns out to
+// be; the blocks of a range, one for each tile of A, run side by side on an XCD and read the same g at the same time.  A block leaves its
+// share of a tile in register order, grad_finish_kernel adds a tile's shares in order.
+struct GradArgs {
+    Product p;
+    int a_tiles;
+    const int32_t *n_rows;
+    int row0, max_rows;
+    int C;
+    float *part;
+    const int32_t *row_of;
+    int H;
+    void *out;
+    float *acc;                     // dV over several chunks of rows
+    int first, last;
+};
+constexpr int kMinStages = 8;       // a range is no shorter
+struct GradPlan {
+    int b_tiles, nk, stages;        // stages of a part product, of a tile
+    int64_t total;
+    int per, ranges;
+};
+__host__ __device__ inline int grad_ranges(int places, int a_tiles) { return places > a_tiles ? places / a_tiles : 1; }      // at most
+template <bool WEIGHTS, int WM>
+__device__ __forceinline__ GradPlan grad_plan(const GradArgs &a) {
+    const int rows = chunk_rows(a.n_rows, a.row0, a.max_rows);
+    GradPlan g;
+    g.b_tiles = WEIGHTS ? (a.C + kTileB - 1) / kTileB : (rows + kTileB - 1) / kTileB;
+    g.nk = WEIGHTS ? (rows + 31) / 32 : (a.C + 31) / 32;
+    g.stages = g.nk * a.p.pairs.n;
+    g.total = (int64_t)g.b_tiles * g.stages;
+    const int most = grad_ranges(kTilePlaces<WM>, a.a_tiles);
+    const int64_t per = (g.total + most - 1) / most;
+    g.per = (int)(per > kMinStages ? per : kMinStages);
+    g.ranges = (int)((g.total + g.per - 1) / g.per);
+    return g;
+}
+template <bool WEIGHTS, int WM>
+__global__ void __launch_bounds__(kTileT<WM>, 4 / WM)
+grad_product_kernel(const GradArgs a) {
+    __shared__ __attribute__((aligned(1024))) char lds[kTileBufs<WM> * kTileBuf<WM>];
+    const GradPlan g = grad_plan<WEIGHTS, WM>(a);
+    const int64_t place = xcd_order((int64_t)g.ranges * a.a_tiles);
+    if (place < 0) return;
+    const int64_t range = place / a.a_tiles;
+    const int at = (int)(place - range * a.a_tiles);
+    int64_t s = range * g.per;
+    const int64_t end = s + g.per < g.total ? s + g.per : g.total;
+    while (s < end) {
+        const int bt = (int)(s / g.stages), s0 = (int)(s - (int64_t)bt * g.stages);
+        const int n = end - s < g.stages - s0 ? (int)(end - s) : g.stages - s0;
+        floatx16 acc[2][4];
+        clear_tile(acc);
+        if constexpr (WEIGHTS) multiply_tile<false, WM>(a.p, (int64_t)at * kTileA<WM>, (int64_t)bt * kTileB, g.nk, s0, n, lds, acc);
+        else multiply_tile<true, WM>(a.p, at * (kTileA<WM> / 32), bt * (kTileB / 32), g.nk, s0, n, lds, acc);
+        float4 *out = reinterpret_cast<float4 *>(a.part + ((bt + range) * a.a_tiles + at) * (kTileA<WM> * kTileB)) + threadIdx.x;
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int v = 0; v < 4; ++v)
+                    out[((i * 4 + j) * 4 + v) * kTileT<WM>] = make_float4(acc[i][j][4 * v], acc[i][j][4 * v + 1], acc[i][j][4 * v + 2], acc[i][j][4 * v + 3]);
+        s += n;
+    }
+}
+// 32 blocks a tile
+template <bool WEIGHTS, int WM, typename O>
+__global__ void __launch_bounds__(kTileT<WM>)
+grad_finish_kernel(const GradArgs a) {
+    const GradPlan g = grad_plan<WEIGHTS, WM>(a);
+    const int tile = blockIdx.x >> 5, rest = blockIdx.x & 31, t = threadIdx.x;
+    const int at = tile % a.a_tiles, bt = tile / a.a_tiles;
+    if (bt >= g.b_tiles) return;
+    const int lane = t & 63, wave = t >> 6, i = rest >> 4, j = (rest >> 2) & 3, v = rest & 3;
+    const int m = at * kTileA<WM> + (wave >> 1) * 64 + i * 32 + v * 8 + (lane >> 5) * 4;     // first of four features
+    const int n = bt * kTileB + (wave & 1) * 128 + j * 32 + (lane & 31);                          // row or class
+    if (m >= a.H || n >= (WEIGHTS ? a.C : chunk_rows(a.n_rows, a.row0, a.max_rows))) return;
+    float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (g.stages > 0) {
+        const int64_t first = (int64_t)bt * g.stages / g.per, last = ((int64_t)(bt + 1) * g.stages - 1) / g.per;
+        const float4 *in = reinterpret_cast<const float4 *>(a.part + ((bt + first) * a.a_tiles + at) * (kTileA<WM> * kTileB)) + rest * kTileT<WM> + t;
+#pragma unroll 4
+        for (int64_t k = first; k <= last; ++k) {
+            const float4 p = in[(k - first) * a.a_tiles * (kTileA<WM> * kTileB / 4)];
+            s[0] += p.x; s[1] += p.y; s[2] += p.z; s[3] += p.w;
+        }
+    }
+    const int64_t to = (WEIGHTS ? (int64_t)n : (int64_t)a.row_of[a.row0 + n]) * a.H + m;
+    const int left = a.H - m < 4 ? a.H - m : 4;
+    if (WEIGHTS && !a.first)
+        for (int k = 0; k < left; ++k) s[k] += a.acc[to + k];
+    if (WEIGHTS && !a.last) {
+        for (int k = 0; k < left; ++k) a.acc[to + k] = s[k];
+        return;
+    }
+    O e[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) e[k] = from_f32<O>(s[k]);
+    O *o = static_cast<O *>(a.out) + to;
+    if (left == 4) {
+        __builtin_memcpy(o, e, sizeof(e));
+    } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (k < left) o[k] = e[k];
+    }
+}
+
+// ---- logits of wide states: both operands stream ---------------------------------------------------------
+// G = 0: A = class weights, B = states; statistics of every 64 classes.  G > 0: A = states, B = class weights; g.
+struct LogitArgs {
+    Product p;
+    int nk, a_tiles, b_tiles;       // (those of the rows are known on the device)
+    const int32_t *n_rows;
+    int row0, max_rows;
+    const float *bias;              // padded with -inf
+    float2 *stat;                   // [2 a_tiles][max_rows]
+    const float *side;              // the rows' records, as in ResArgs
+    char *g; int64_t g_slab, g_part;
+    float *db_part;                 // [2 row tiles][256 b_tiles]
+};
+template <int G, bool CLOSE>
+__global__ void __launch_bounds__(kTileT<2>, 2)
+wide_logits_kernel(const LogitArgs a) {
+    __shared__ __attribute__((aligned(1024))) char lds[kTileBufs<2> * kTileBuf<2>];
+    const int rows = chunk_rows(a.n_rows, a.row0, a.max_rows);
+    const int row_tiles = (rows + 255) / 256 * (G == 0 ? 1 : 2), class_tiles = G == 0 ? a.a_tiles : a.b_tiles;
+    const int64_t i = xcd_order((int64_t)row_tiles * class_tiles);
+    if (i < 0) return;
+    // bands of eight row tiles, class tiles one after another inside a band: the blocks of an XCD share them in its L2
+    const int band = (int)(i / (8 * (int64_t)class_tiles)), rem = (int)(i - (int64_t)band * 8 * class_tiles);
+    const int left = row_tiles - band * 8, width = left < 8 ? left : 8;
+    const int ct = rem / width, rt = band * 8 + rem % width;
+    floatx16 acc[2][4];
+    clear_tile(acc);
+    const int n_stages = a.nk * a.p.pairs.n;
+    multiply_tile<false, 2>(a.p, (int64_t)(G == 0 ? ct : rt) * 128, (int64_t)(G == 0 ? rt : ct) * 256, a.nk, 0, n_stages, lds, acc);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave >> 1, wn = wave & 1, hf = lane >> 5, l32 = lane & 31;
+    if constexpr (G == 0) {
+        const int c0 = ct * 128 + wm * 64;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const float4 b = *reinterpret_cast<const float4 *>(a.bias + c0 + t * 32 + q * 8 + hf * 4);
+                const float e[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) acc[t][j][4 * q + k] += e[k];
+            }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int r = rt * 256 + wn * 128 + j * 32 + l32;
+            float top = -INFINITY;
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) top = fmaxf(top, acc[t][j][v]);
+            top = fmaxf(top, __shfl_xor(top, 32));
+            const float from = top == -INFINITY ? 0.0f : top;       // every class masked: the sum is 0, not NaN
+            float s = 0.0f;
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) s += CLOSE ? exp_close(acc[t][j][v] - from) : __expf(acc[t][j][v] - from);
+            s += __shfl_xor(s, 32);
+            if (hf == 0) a.stat[(int64_t)(2 * ct + wm) * a.max_rows + r] = make_float2(from, s);
+        }
+    } else {
+        const int c0 = ct * 256 + wn * 128 + l32, r0 = rt * 128 + wm * 64;
+        float colsum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        float own_bias[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) own_bias[j] = a.bias[c0 + j * 32];
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const float *rec = a.side + (int64_t)(r0 / 32 + t) * 128 + q * 8 + hf * 4;
+                const float4 l4 = *reinterpret_cast<const float4 *>(rec), w4 = *reinterpret_cast<const float4 *>(rec + 32);
+                const int4 n4 = *reinterpret_cast<const int4 *>(rec + 64);
+                const float lse[4] = {l4.x, l4.y, l4.z, l4.w}, w[4] = {w4.x, w4.y, w4.z, w4.w};
+                const int label[4] = {n4.x, n4.y, n4.z, n4.w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    float d[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float z = acc[t][j][4 * q + e] + own_bias[j];
+                        const float p = CLOSE ? exp_close(z - lse[e]) : __builtin_amdgcn_exp2f(fmaf(z, kLog2e, -lse[e]));
+                        d[e] = (p - (label[e] == c0 + j * 32 ? 1.0f : 0.0f)) * w[e];
+                        colsum[j] += d[e];
+                    }
+#pragma unroll
+                    for (int k = 0; k < G; ++k) {
+                        const u32x2 y = {pack_bf16(d[0], d[1]), pack_bf16(d[2], d[3])};
+                        __builtin_memcpy(a.g + k * a.g_part + (int64_t)(r0 / 32 + t) * a.g_slab + (int64_t)(c0 + j * 32) * 64 + q * 16 + hf * 8, &y, 8);
+                        d[0] -= low_bf16(y[0]); d[1] -= high_bf16(y[0]); d[2] -= low_bf16(y[1]); d[3] -= high_bf16(y[1]);
+                    }
+                }
+            }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float s = colsum[j] + __shfl_xor(colsum[j], 32);
+            if (hf == 0) a.db_part[((int64_t)(rt * 2 + wm) * a.b_tiles) * 256 + c0 + j * 32] = s;
+        }
+    }
+}
+
+}  // namespace
+}  // namespace jitdb
