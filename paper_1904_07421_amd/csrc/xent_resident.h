@@ -25,6 +25,7 @@ constexpr int kResTile = 32;             // rows of the other operand in a tile
 constexpr int kResBufs = 3;
 constexpr int kResMinTiles = 8;          // a block's range is no shorter
 constexpr int kResBlocks = 1024;         // ranges make no more blocks than this
+constexpr int kResInAcc = 44;            // resident fragments that are kept in accumulation registers, of 64 at most
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
 struct ResArgs {
@@ -144,6 +145,16 @@ resident_kernel(const ResArgs a) {
 #pragma unroll
             for (int k = 0; k < KS; ++k)
                 hb[p][j][k] = *reinterpret_cast<const u32x4 *>(a.res + (int64_t)(p * (KS / 2) + k / 2) * a.res_slab + (int64_t)(r0 + j * 32 + l32) * 64 + (k & 1) * 32 + hf * 16);
+    // Most of them in accumulation registers, from where the matrix instructions take them as well: left to itself the compiler moves
+    // them there and back.
+    if constexpr (ALONE)
+#pragma unroll
+        for (int p = 0; p < PARTS; ++p)
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int k = 0; k < KS; ++k)
+                    if ((p * 2 + j) * KS + k < kResInAcc) asm volatile("" : "+a"(hb[p][j][k]));
     float own_bias[2] = {0.0f, 0.0f};
     if constexpr (G != 0) {
         own_bias[0] = a.bias[r0 + l32];
@@ -197,7 +208,7 @@ resident_kernel(const ResArgs a) {
     // Statistics: sums of exp(z - ref).  The reference is the maximum of the tiles up to the last one that left the range of fp32
     // (the first does): only then is a maximum taken and the sum so far scaled.
     float ref[2] = {-INFINITY, -INFINITY}, ref_l[2] = {0.0f, 0.0f}, sum[2] = {__builtin_nanf(""), __builtin_nanf("")}, kept[2] = {0.0f, 0.0f};
-    float late[2] = {0.0f, 0.0f};                        // an exponential is added one product after it is asked for
+    float late[2] = {0.0f, 0.0f}, arg = 0.0f;            // an exponential is added when the tile's next is asked for
     // Derivatives
     float colsum[2] = {0.0f, 0.0f};
     uint32_t words[G > 0 ? G : 1][2][2];                 // [part][q & 1][pair]
@@ -206,15 +217,19 @@ resident_kernel(const ResArgs a) {
     char *g_lane = a.g + (int64_t)(r0 + l32) * 64 + hf * 16;
 
     auto statistics = [&](auto s_tag, floatx16 (&z)[2]) __attribute__((always_inline)) {
-        constexpr int S = decltype(s_tag)::value, E0 = (S * 32 + SLOTS - 1) / SLOTS, E1 = ((S + 1) * 32 + SLOTS - 1) / SLOTS;
-#pragma unroll
-        for (int e = E0; e < E1; ++e) {
-            const int j = e & 1, v = e >> 1;
-            if constexpr (ALONE) asm volatile("" : "+a"(z[j]));          // the accumulator is fetched here, not all of them in front of the tile
-            const float x = z[j][v];
-            sum[j] += late[j];
-            late[j] = CLOSE ? exp_close(x - ref[j]) : __builtin_amdgcn_exp2f(fmaf(x, kLog2e, -ref_l[j]));
-        }
+        constexpr int S = decltype(s_tag)::value;
+        // step 2 e fetches and scales element e, step 2 e + 1 asks for its exponential and adds the one before
+        constexpr int E0 = S * 64 / SLOTS, E1 = (S + 1) * 64 / SLOTS;
+        static_for<E1 - E0>([&](auto e_tag) __attribute__((always_inline)) {
+            constexpr int E = (E0 + decltype(e_tag)::value) >> 1, J = E & 1, V = E >> 1;
+            if constexpr ((E0 + decltype(e_tag)::value) % 2 == 0) {
+                if constexpr (ALONE) asm volatile("" : "+a"(z[J]));      // the accumulator is fetched here, not all of them in front of the tile
+                arg = CLOSE ? z[J][V] - ref[J] : fmaf(z[J][V], kLog2e, -ref_l[J]);
+            } else {
+                sum[J] += late[J];
+                late[J] = CLOSE ? exp_close(arg) : __builtin_amdgcn_exp2f(arg);
+            }
+        });
     };
     auto statistics_end = [&](floatx16 (&z)[2]) __attribute__((always_inline)) {
 #pragma unroll
