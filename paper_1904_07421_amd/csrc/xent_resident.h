@@ -86,20 +86,24 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) { return __built
 __device__ __forceinline__ float low_bf16(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float high_bf16(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 
+// products (for both resident tiles) of a tile's first fragments
+template <int PARTS>
+constexpr int res_products(int fragments) { return PARTS == 3 ? fragments / 3 * 12 + (fragments % 3 == 0 ? 0 : fragments % 3 == 1 ? 2 : 6) : fragments * 2; }
+
 // PARTS: bf16 parts of both operands; KS: K in steps of 16; G: 0 = statistics, else g in that many parts.
 template <int PARTS, int KS, int G>
 __global__ void __launch_bounds__(kResT, res_alone(PARTS * KS, G > 0) ? 1 : 2)
 resident_kernel(const ResArgs a) {
     constexpr int NF = PARTS * KS;                       // fragments of a tile, 1 KB each
-    constexpr int NG = (NF + 3) / 4;                     // groups of four
+    constexpr int NG = NF / 2;                           // groups of two
+    constexpr int RING = NG % 3 == 0 ? 3 : 4;            // groups of fragments in registers: one multiplied, two on their way
     constexpr int SIDE = G == 0 ? 1 : 2;                 // loads of what comes with a tile, 256 bytes each, a copy for each wave
     constexpr int LOADS = (NF + 3) / 4 + SIDE;           // per wave and tile
     constexpr int BUF = NF * 1024 + 4 * SIDE * 256;
     constexpr int PRODUCTS = PARTS == 3 ? KS * 12 : KS * 2;       // of a tile and wave
-    // of those, the ones that work is dealt out over: for g, those in front of the last two groups, which read the next rows' values
-    constexpr int BEFORE_TWO = (NG - 2) * 4;             // fragments
-    constexpr int SLOTS = G == 0 || !res_alone(NF, G > 0) ? PRODUCTS
-                          : PARTS == 3 ? BEFORE_TWO / 3 * 12 + (BEFORE_TWO % 3 == 0 ? 0 : BEFORE_TWO % 3 == 1 ? 2 : 6) : BEFORE_TWO * 2;
+    // of those, the ones that work is dealt out over: for g, those in front of the last three groups, in which the next rows' values come
+    constexpr int EARLY = (NG - 3) * 2;                  // fragments
+    constexpr int SLOTS = G == 0 || !res_alone(NF, G > 0) ? PRODUCTS : res_products<PARTS>(EARLY);
     constexpr bool ALONE = res_alone(NF, G > 0);
     constexpr bool CLOSE = PARTS == 3 || G == 3;         // fp32 results: exponentials good to a rounding
     __shared__ __attribute__((aligned(1024))) char lds[kResBufs * BUF];
@@ -117,21 +121,23 @@ resident_kernel(const ResArgs a) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), hf = lane >> 5, l32 = lane & 31;
     const int r0 = rb * kResRows + wave * 64;            // the wave's first resident row
     // ---- movers: 1 KB units of 16 rows of a slab, piece p of row r in slot p ^ ((r >> 2) & 3)
-    const char *str_lane = a.str + (lane >> 2) * 64 + (((lane & 3) ^ ((lane >> 4) & 3)) * 16);
-    const float *side_lane = a.side + lane;
-    auto issue = [&](int tile, int buf) __attribute__((always_inline)) {
+    // (scalar addresses and one offset for every lane: no vector instruction is spent on them)
+    const uint32_t str_lane = (lane >> 2) * 64 + (((lane & 3) ^ ((lane >> 4) & 3)) * 16), side_lane = lane * 4;
+    auto issue_one = [&](int tile, int buf, int i) __attribute__((always_inline)) {
         char *dst = lds + buf * BUF;
-#pragma unroll
-        for (int i = 0; i < LOADS - SIDE; ++i) {
+        if (i < LOADS - SIDE) {
             int u = wave + 4 * i;
             if (NF % 4 != 0 && u >= NF) u = NF - 1;      // the same bytes to the same place once more: every wave issues as many
-            __builtin_amdgcn_global_load_lds(JITDB_GLOBAL_PTR(str_lane + (int64_t)(u >> 1) * a.str_slab + (int64_t)tile * 2048 + (u & 1) * 1024),
-                                             JITDB_LDS_PTR(dst + u * 1024), 16, 0, 0);
+            const char *at = a.str + (int64_t)(u >> 1) * a.str_slab + (int64_t)tile * 2048 + (u & 1) * 1024;
+            __builtin_amdgcn_global_load_lds(JITDB_GLOBAL_PTR(at + str_lane), JITDB_LDS_PTR(dst + u * 1024), 16, 0, 0);
+        } else {
+            const char *at = reinterpret_cast<const char *>(a.side) + (int64_t)tile * (G == 0 ? 128 : 512) + (i - (LOADS - SIDE)) * 256;
+            __builtin_amdgcn_global_load_lds(JITDB_GLOBAL_PTR(at + side_lane), JITDB_LDS_PTR(dst + NF * 1024 + (wave * SIDE + i - (LOADS - SIDE)) * 256), 4, 0, 0);
         }
+    };
+    auto issue = [&](int tile, int buf) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < SIDE; ++i)
-            __builtin_amdgcn_global_load_lds(JITDB_GLOBAL_PTR(side_lane + (int64_t)tile * (G == 0 ? 32 : 128) + i * 64),
-                                             JITDB_LDS_PTR(dst + NF * 1024 + (wave * SIDE + i) * 256), 4, 0, 0);
+        for (int i = 0; i < LOADS; ++i) issue_one(tile, buf, i);
     };
     auto wait_barrier = [&](auto n) __attribute__((always_inline)) {
         asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(decltype(n)::value) : "memory");
@@ -171,18 +177,15 @@ resident_kernel(const ResArgs a) {
 #pragma unroll
     for (int k = 0; k < 2; ++k) rd[k] = lds_base + l32 * 64 + (((2 * k + hf) ^ ((l32 >> 2) & 3)) * 16);
     const uint32_t rd_side = lds_base + NF * 1024 + wave * SIDE * 256 + hf * 16, rd_label = rd_side - hf * 16 + 256 + l32 * 4;
-    u32x4 fa[2][4], side[4];                             // side: G = 0, the bias of the next tile's 16 classes of this lane
+    u32x4 fa[RING][2], side[4];                            // side: G = 0, the bias of the next tile's 16 classes of this lane
     u32x4 lse_w[2][4];                                   // G > 0: log-sum-exp and weight of 16 rows of the tile that is worked on
     int32_t label = -1;                                  // ... label of row l32
     // fragment f of a tile: K step f / PARTS, part PARTS - 1 - f % PARTS (the smallest first)
-    auto read_group = [&](auto g_tag, uint32_t at, u32x4 (&f)[4]) __attribute__((always_inline)) {
+    auto read_group = [&](auto g_tag, uint32_t at, u32x4 (&f)[2]) __attribute__((always_inline)) {
         constexpr int GI = decltype(g_tag)::value;
-        static_for<4>([&](auto i_tag) __attribute__((always_inline)) {
-            constexpr int F = GI * 4 + decltype(i_tag)::value;
-            if constexpr (F < NF) {
-                constexpr int K = F / PARTS, P = PARTS - 1 - F % PARTS;
-                lds_read16<(P * (KS / 2) + K / 2) * 2048>(f[decltype(i_tag)::value], rd[K & 1] + at);
-            }
+        static_for<2>([&](auto i_tag) __attribute__((always_inline)) {
+            constexpr int F = GI * 2 + decltype(i_tag)::value, K = F / PARTS, P = PARTS - 1 - F % PARTS;
+            lds_read16<(P * (KS / 2) + K / 2) * 2048>(f[decltype(i_tag)::value], rd[K & 1] + at);
         });
     };
     auto read_bias = [&](uint32_t at) __attribute__((always_inline)) {
@@ -195,12 +198,16 @@ resident_kernel(const ResArgs a) {
         });
         lds_read4(label, rd_label + at);
     };
-    auto reads_done = [&](u32x4 (&f)[4]) __attribute__((always_inline)) {
+    // at most `later` reads asked for after these are still on their way
+    auto reads_done = [&](auto later, u32x4 (&f)[2]) __attribute__((always_inline)) {
+        asm volatile("s_waitcnt lgkmcnt(%2)" : "+v"(f[0]), "+v"(f[1]) : "n"(decltype(later)::value));
+    };
+    auto four_done = [&](u32x4 (&f)[4]) __attribute__((always_inline)) {
         asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(f[0]), "+v"(f[1]), "+v"(f[2]), "+v"(f[3]));
     };
     auto rows_done = [&]() __attribute__((always_inline)) {
-        reads_done(lse_w[0]);
-        reads_done(lse_w[1]);
+        four_done(lse_w[0]);
+        four_done(lse_w[1]);
         asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(label));
     };
 
@@ -330,17 +337,19 @@ resident_kernel(const ResArgs a) {
     int buf = 0;
     wait_barrier(younger_first);
     read_group(std::integral_constant<int, 0>(), 0, fa[0]);
+    read_group(std::integral_constant<int, 1>(), 0, fa[1]);
     if constexpr (G == 0 && ALONE) {
         read_bias(0);
-        reads_done(side);
+        four_done(side);
     }
-    reads_done(fa[0]);
+    reads_done(std::integral_constant<int, 0>(), fa[0]);
     // One tile: its products into `now`; the tile before, in `before`, is worked on between them if EARLIER
     auto walk = [&](auto turn_tag, auto earlier_tag, int i, floatx16 (&now)[2], floatx16 (&before)[2]) __attribute__((always_inline)) {
         constexpr int TURN = decltype(turn_tag)::value;
         constexpr bool EARLIER = decltype(earlier_tag)::value;
         const uint32_t at = buf * BUF;
         const int next_buf = buf == kResBufs - 1 ? 0 : buf + 1;
+        const int ahead = t0 + (i + kResBufs < n_tiles ? i + kResBufs : n_tiles - 1);
         floatx16 start;
         if constexpr (G == 0 && !ALONE) {                // (the other wave has the SIMD meanwhile)
             const uint32_t from = rd_side + at;
@@ -351,46 +360,47 @@ resident_kernel(const ResArgs a) {
 #pragma unroll
             for (int v = 0; v < 16; ++v) start[v] = __uint_as_float(side[v >> 2][v & 3]);
         static_for<NG>([&](auto g_tag) __attribute__((always_inline)) {
-            constexpr int GI = decltype(g_tag)::value, CUR = (TURN * NG + GI) & 1;
-            if constexpr (GI == NG - 1) {
+            constexpr int GI = decltype(g_tag)::value, COUNT = TURN * NG + GI, CUR = COUNT % RING, NEXT = (COUNT + 1) % RING, AFTER = (COUNT + 2) % RING;
+            if constexpr (G != 0 && GI == NG - 3) {
+                if constexpr (ALONE && EARLIER) derivatives_end(before, t0 + i - 1);
+                read_rows(at);
+            }
+            if constexpr (GI == NG - 2) {
                 // this tile's buffer has been read: it takes the tile three on; the next tile is there
                 wait_barrier(younger);
-                issue(t0 + (i + kResBufs < n_tiles ? i + kResBufs : n_tiles - 1), buf);
+                if constexpr (G != 0) rows_done();
                 if constexpr (G == 0 && ALONE) read_bias(next_buf * BUF);
-                read_group(std::integral_constant<int, 0>(), next_buf * BUF, fa[CUR ^ 1]);
-            } else {
-                if constexpr (G != 0 && GI == NG - 2) {
-                    if constexpr (ALONE && EARLIER) derivatives_end(before, t0 + i - 1);
-                    read_rows(at);
-                }
-                read_group(std::integral_constant<int, GI + 1>(), at, fa[CUR ^ 1]);
             }
+            if constexpr (GI < NG - 2) read_group(std::integral_constant<int, GI + 2>(), at, fa[AFTER]);
+            else read_group(std::integral_constant<int, GI + 2 - NG>(), next_buf * BUF, fa[AFTER]);
             __builtin_amdgcn_sched_barrier(0);
-            static_for<4>([&](auto f_tag) __attribute__((always_inline)) {
-                constexpr int F = GI * 4 + decltype(f_tag)::value;
-                if constexpr (F < NF) {
-                    constexpr int K = F / PARTS, P = PARTS - 1 - F % PARTS;
-                    static_for<(PARTS - P) * 2>([&](auto m_tag) __attribute__((always_inline)) {
-                        constexpr int M = decltype(m_tag)::value, J = M & 1, PB = PARTS - 1 - P - M / 2;
-                        constexpr int S = PARTS == 3 ? K * 12 + (P == 2 ? 0 : P == 1 ? 2 : 6) + M : F * 2 + M;
-                        if constexpr (S < 2 && G == 0) now[J] = start;
-                        if constexpr (S < 2 && G != 0)
+            static_for<2>([&](auto f_tag) __attribute__((always_inline)) {
+                constexpr int F = GI * 2 + decltype(f_tag)::value, K = F / PARTS, P = PARTS - 1 - F % PARTS;
+                static_for<(PARTS - P) * 2>([&](auto m_tag) __attribute__((always_inline)) {
+                    constexpr int M = decltype(m_tag)::value, J = M & 1, PB = PARTS - 1 - P - M / 2;
+                    constexpr int S = PARTS == 3 ? K * 12 + (P == 2 ? 0 : P == 1 ? 2 : 6) + M : F * 2 + M;
+                    if constexpr (S < 2 && G == 0) now[J] = start;
+                    if constexpr (S < 2 && G != 0)
 #pragma unroll
-                            for (int v = 0; v < 16; ++v) now[J][v] = own_bias[J];
-                        mfma_step<bf16_t>(fa[CUR][decltype(f_tag)::value], hb[PB][J][K], now[J]);
-                        if constexpr (ALONE && EARLIER && S < SLOTS) {
-                            __builtin_amdgcn_sched_barrier(0);
-                            if constexpr (G == 0) statistics(std::integral_constant<int, S>(), before);
-                            else derivatives(std::integral_constant<int, S>(), before, t0 + i - 1);
-                            __builtin_amdgcn_sched_barrier(0);
-                        }
-                    });
-                }
+                        for (int v = 0; v < 16; ++v) now[J][v] = own_bias[J];
+                    mfma_step<bf16_t>(fa[CUR][decltype(f_tag)::value], hb[PB][J][K], now[J]);
+                    __builtin_amdgcn_sched_barrier(0);
+                    // the requests go out between the last products, not in one burst
+                    constexpr int LAST = PRODUCTS - res_products<PARTS>((NG - 2) * 2), L0 = PRODUCTS - LAST, FROM = (S - L0) * LOADS / LAST, TO = (S - L0 + 1) * LOADS / LAST;
+                    if constexpr (S >= L0)
+#pragma unroll
+                        for (int l = FROM; l < TO; ++l) issue_one(ahead, buf, l);
+                    if constexpr (ALONE && EARLIER && S < SLOTS) {
+                        if constexpr (G == 0) statistics(std::integral_constant<int, S>(), before);
+                        else derivatives(std::integral_constant<int, S>(), before, t0 + i - 1);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                });
             });
-            __builtin_amdgcn_sched_barrier(0);
-            if constexpr (G == 0 && ALONE && GI == NG - 1) reads_done(side);
-            if constexpr (G != 0 && GI == NG - 2) rows_done();
-            reads_done(fa[CUR ^ 1]);
+            // the next group is there (behind it at most the one after, and the rows' values)
+            if constexpr (GI == NG - 3 && G != 0) reads_done(std::integral_constant<int, 11>(), fa[NEXT]);
+            else reads_done(std::integral_constant<int, 2>(), fa[NEXT]);
+            if constexpr (G == 0 && ALONE && GI == NG - 1) four_done(side);
         });
         buf = next_buf;
         if constexpr (ALONE && EARLIER && G == 0) statistics_end(before);
@@ -404,6 +414,12 @@ resident_kernel(const ResArgs a) {
         if constexpr (G == 0) statistics_end(last);
         else derivatives_end(last, tile);
     };
+    // The fragments that were asked for behind the last tile arrive before their registers are anybody else's.
+    auto drain = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int r = 0; r < RING; ++r) reads_done(std::integral_constant<int, 0>(), fa[r]);
+        if constexpr (G == 0 && ALONE) four_done(side);
+    };
     const std::integral_constant<int, 0> turn0;
     const std::integral_constant<int, 1> turn1;
     if constexpr (ALONE) {
@@ -415,16 +431,20 @@ resident_kernel(const ResArgs a) {
         }
         if (i < n_tiles) {
             walk(turn1, std::true_type(), i, zb, za);
+            drain();
             finish(zb, t1 - 1);
         } else {
+            drain();
             finish(za, t1 - 1);
         }
     } else {
-        static_assert(ALONE || NG % 2 == 0, "the fragments of the next tile's first group end up in the buffer it starts with");
+        static_assert(ALONE || NG % RING == 0, "the fragments of the next tile's first group end up where it starts");
+    static_assert(2 * NG % RING == 0, "... of the tile after the next");
         for (int i = 0; i < n_tiles; ++i) {
             walk(turn0, std::false_type(), i, za, za);
             finish(za, t0 + i);
         }
+        drain();
     }
     if constexpr (G == 0) {
 #pragma unroll

@@ -55,7 +55,9 @@ __device__ __forceinline__ void multiply_tile(const Product &p, int64_t a0, int6
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave >> 1, wn = wave & 1, hf = lane >> 5, l32 = lane & 31, lrow = lane >> 2;
-    // movers: 1 KB units of 16 rows of a slab, those of A in front of those of B, LOADS a wave
+    // movers: 1 KB units of 16 rows of a slab, those of A in front of those of B, LOADS a wave (scalar addresses and one offset for
+    // every lane: no vector instruction is spent on them)
+    const uint32_t lane_off = lrow * 64 + (K_ROWS ? lane & 3 : (lane & 3) ^ ((lane >> 4) & 3)) * 16;
     const char *from[LOADS];
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
@@ -65,9 +67,9 @@ __device__ __forceinline__ void multiply_tile(const Product &p, int64_t a0, int6
         if constexpr (K_ROWS) {
             const int n_slabs = u < A_UNITS ? p.a_slabs : p.b_slabs;
             const int64_t s = first + (v >> 1) < n_slabs ? first + (v >> 1) : n_slabs - 1;
-            from[i] = o.at + s * o.slab + ((v & 1) * 16 + lrow) * 64 + (lane & 3) * 16;
+            from[i] = o.at + s * o.slab + (v & 1) * 1024;
         } else {
-            from[i] = o.at + (first + v * 16 + lrow) * 64 + ((lane & 3) ^ ((lane >> 4) & 3)) * 16;
+            from[i] = o.at + (first + v * 16) * 64;
         }
     }
     const int64_t a_stage = K_ROWS ? 32 * 64 : p.A.slab, b_stage = K_ROWS ? 32 * 64 : p.B.slab;
@@ -75,7 +77,8 @@ __device__ __forceinline__ void multiply_tile(const Product &p, int64_t a0, int6
     int64_t a_off = p.pairs.a[q] + k * a_stage, b_off = p.pairs.b[q] + k * b_stage;
     auto issue_one = [&](int buf, int i) __attribute__((always_inline)) {
         const int u = wave * LOADS + i;
-        __builtin_amdgcn_global_load_lds(JITDB_GLOBAL_PTR(from[i] + (u < A_UNITS ? a_off : b_off)), JITDB_LDS_PTR(lds + buf * BUF + u * 1024), 16, 0, 0);
+        const char *at = from[i] + (u < A_UNITS ? a_off : b_off);
+        __builtin_amdgcn_global_load_lds(JITDB_GLOBAL_PTR(at + lane_off), JITDB_LDS_PTR(lds + buf * BUF + u * 1024), 16, 0, 0);
     };
     auto advance = [&]() __attribute__((always_inline)) {        // behind the last stage the last one is asked for again: the waits count on it
         if (++issued >= n_stages) return;
