@@ -68,27 +68,66 @@ __device__ __forceinline__ void apply_drop(const Drop &d, uint64_t start, uint64
     for (int k = 0; k < N; ++k) v[k] = u[k] >= d.limit && !d.all ? v[k] * d.scale : 0.0f;
 }
 
-// VEC elements of 16 bytes, from any element boundary; only the first `left` exist
+// Sixteen bytes of a row, from any element boundary; only the first `left` elements exist.  Loads stay packed until they are used,
+// so that several are on their way; what is written is not read again soon and goes past the caches.
 template <typename T> constexpr int kVec = 16 / (int)sizeof(T);
-template <typename T, int N>
-__device__ __forceinline__ void load_row_piece(const T *p, int left, float (&v)[N]) {
-    T e[N];
+typedef u32x4 __attribute__((aligned(2))) any4;
+template <typename T>
+__device__ __forceinline__ u32x4 load_piece(const T *p, int left) {
+    constexpr int N = kVec<T>;
+    u32x4 w = {0u, 0u, 0u, 0u};
     if (left >= N) {
-        __builtin_memcpy(e, p, sizeof(e));
+        __builtin_memcpy(&w, p, 16);
     } else {
+        T e[N];
 #pragma unroll
         for (int k = 0; k < N; ++k) e[k] = k < left ? p[k] : T(0);
+        __builtin_memcpy(&w, e, 16);
     }
+    return w;
+}
+template <typename E, int N> struct Piece { uint32_t w[N * (int)sizeof(E) / 4]; };
+template <typename E, int N>
+__device__ __forceinline__ Piece<E, N> load_row(const E *p, int left) {
+    Piece<E, N> r = {};
+    if (left >= N) {
+        __builtin_memcpy(&r, p, sizeof(r));
+    } else {
+        E e[N];
 #pragma unroll
-    for (int k = 0; k < N; ++k) v[k] = to_f32<T>(e[k]);
+        for (int k = 0; k < N; ++k) e[k] = k < left ? p[k] : E(0);
+        __builtin_memcpy(&r, e, sizeof(r));
+    }
+    return r;
+}
+template <typename E, int N>
+__device__ __forceinline__ void unpack(const Piece<E, N> &r, float (&v)[N]) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        if constexpr (sizeof(E) == 4) v[k] = __uint_as_float(r.w[k]);
+        else v[k] = __uint_as_float(k & 1 ? r.w[k >> 1] & 0xFFFF0000u : r.w[k >> 1] << 16);
+    }
+}
+template <typename T>
+__device__ __forceinline__ float element(const u32x4 &w, int k) {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(w[k]);
+    else return __uint_as_float(k & 1 ? w[k >> 1] & 0xFFFF0000u : w[k >> 1] << 16);
 }
 template <typename T, int N>
 __device__ __forceinline__ void store_row_piece(T *p, int left, const float (&v)[N]) {
     T e[N];
 #pragma unroll
-    for (int k = 0; k < N; ++k) e[k] = from_f32<T>(v[k]);
+    for (int k = 0; k < N; ++k) {
+        if constexpr (sizeof(T) == 4) e[k] = v[k];
+        else e[k] = __builtin_bit_cast(bf16_t, (__bf16)v[k]);          // (the hardware's rounding, two a instruction)
+    }
     if (left >= N) {
-        __builtin_memcpy(p, e, sizeof(e));
+#pragma unroll
+        for (int q = 0; q < N / kVec<T>; ++q) {
+            u32x4 w;
+            __builtin_memcpy(&w, e + q * kVec<T>, 16);
+            __builtin_nontemporal_store(w, reinterpret_cast<any4 *>(p + q * kVec<T>));
+        }
     } else {
 #pragma unroll
         for (int k = 0; k < N; ++k)
@@ -97,18 +136,30 @@ __device__ __forceinline__ void store_row_piece(T *p, int left, const float (&v)
 }
 
 // ---- dropout ---------------------------------------------------------------------------------
+// Four pieces a thread and turn.
 template <typename T>
 __global__ void __launch_bounds__(kT)
 dropout_kernel(const T *x, int64_t n, const Drop d, T *y) {
-    constexpr int V = kVec<T>;
+    constexpr int V = kVec<T>, TURN = 4;
     const uint64_t start = drop_start(d);
-    const int64_t step = (int64_t)gridDim.x * kT * V;
-    for (int64_t i = ((int64_t)blockIdx.x * kT + threadIdx.x) * V; i < n; i += step) {
-        const int left = n - i < V ? (int)(n - i) : V;
-        float v[V];
-        load_row_piece<T, V>(x + i, left, v);
-        apply_drop<V>(d, start, (uint64_t)i, v);
-        store_row_piece<T, V>(y + i, left, v);
+    const int64_t step = (int64_t)gridDim.x * kT * V * TURN;
+    for (int64_t i0 = ((int64_t)blockIdx.x * kT * TURN + threadIdx.x) * V; i0 < n; i0 += step) {
+        u32x4 w[TURN];
+#pragma unroll
+        for (int u = 0; u < TURN; ++u) {
+            const int64_t i = i0 + (int64_t)u * kT * V;
+            w[u] = load_piece<T>(x + i, n - i >= V ? V : n > i ? (int)(n - i) : 0);
+        }
+#pragma unroll
+        for (int u = 0; u < TURN; ++u) {
+            const int64_t i = i0 + (int64_t)u * kT * V;
+            if (i >= n) break;
+            float v[V];
+#pragma unroll
+            for (int k = 0; k < V; ++k) v[k] = element<T>(w[u], k);
+            apply_drop<V>(d, start, (uint64_t)i, v);
+            store_row_piece<T, V>(y + i, n - i < V ? (int)(n - i) : V, v);
+        }
     }
 }
 
@@ -167,13 +218,26 @@ layernorm_kernel(const NormArgs a) {
             beta[j][k] = c + k < H ? a.beta[c + k] : 0.0f;
         }
     }
-    for (int64_t row = (int64_t)blockIdx.x * GROUPS + threadIdx.x / G; row < a.n; row += (int64_t)gridDim.x * GROUPS) {
-        float v[NV][V];
-        float s = 0.0f;
+    // the next row is on its way while this one is worked on
+    const int64_t step = (int64_t)gridDim.x * GROUPS;
+    int64_t row = (int64_t)blockIdx.x * GROUPS + threadIdx.x / G;
+    Piece<T, V> next[NV];
+    auto fetch = [&](int64_t r) __attribute__((always_inline)) {
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             const int c = (j * G + l) * V;
-            load_row_piece<T, V>(x + row * H + c, H - c, v[j]);
+            next[j] = load_row<T, V>(x + r * H + c, H - c);
+        }
+    };
+    if (row < a.n) fetch(row);
+    for (; row < a.n; row += step) {
+        float v[NV][V];
+#pragma unroll
+        for (int j = 0; j < NV; ++j) unpack<T, V>(next[j], v[j]);
+        if (row + step < a.n) fetch(row + step);
+        float s = 0.0f;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
 #pragma unroll
             for (int k = 0; k < V; ++k) s += v[j][k];
         }
@@ -219,6 +283,7 @@ layernorm_backward_kernel(const NormArgs a) {
     const uint64_t start = a.drop.state ? drop_start(a.drop) : 0;
     // gamma and the gradients of the longest rows do not fit the registers of 512 threads: the gradients stay in LDS
     constexpr bool KEEP = G <= 64;
+    constexpr bool AHEAD = G <= 64 && NV * V <= 16;      // the next row is on its way while this one is worked on, where registers allow
     float gamma[KEEP ? NV : 1][V], dgamma[KEEP ? NV : 1][V], dbeta[KEEP ? NV : 1][V];
 #pragma unroll
     for (int j = 0; j < NV; ++j)
@@ -232,16 +297,37 @@ layernorm_backward_kernel(const NormArgs a) {
                 sums[c] = sums[W + c] = 0.0f;
             }
         }
-    for (int64_t row = (int64_t)blockIdx.x * GROUPS + threadIdx.x / G; row < a.n; row += (int64_t)gridDim.x * GROUPS) {
+    const int64_t step = (int64_t)gridDim.x * GROUPS;
+    int64_t row = (int64_t)blockIdx.x * GROUPS + threadIdx.x / G;
+    Piece<T, V> next_x[NV];
+    Piece<GT, V> next_g[NV];
+    float next_mean = 0.0f, next_rstd = 0.0f;
+    auto fetch = [&](int64_t r) __attribute__((always_inline)) {
+        next_mean = a.mean[r];
+        next_rstd = a.rstd[r];
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int c = (j * G + l) * V;
+            next_x[j] = load_row<T, V>(x + r * H + c, H - c);
+            next_g[j] = load_row<GT, V>(gy + r * H + c, H - c);
+        }
+    };
+    if (AHEAD && row < a.n) fetch(row);
+    for (; row < a.n; row += step) {
+        if constexpr (!AHEAD) fetch(row);
         if constexpr (!KEEP) asm volatile("" : "+v"(l));        // addresses and gamma anew for each row: kept, they cost registers
         float xh[NV][V], g[NV][V];
-        const float mean = a.mean[row], rstd = a.rstd[row];
+        const float mean = next_mean, rstd = next_rstd;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            unpack<T, V>(next_x[j], xh[j]);
+            unpack<GT, V>(next_g[j], g[j]);
+        }
+        if (AHEAD && row + step < a.n) fetch(row + step);
         float s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             const int c = (j * G + l) * V;
-            load_row_piece<T, V>(x + row * H + c, H - c, xh[j]);
-            load_row_piece<GT, V>(gy + row * H + c, H - c, g[j]);
             if (a.drop.state) apply_drop<V>(a.drop, start, (uint64_t)row * H + c, g[j]);
 #pragma unroll
             for (int k = 0; k < V; ++k) {
@@ -268,14 +354,7 @@ layernorm_backward_kernel(const NormArgs a) {
             if (c >= H) continue;
 #pragma unroll
             for (int k = 0; k < V; ++k) g[j][k] = (g[j][k] - s1 - xh[j][k] * s2) * rstd;
-            float *o = a.dx + row * H + c;
-            if (c + V <= H) {
-                __builtin_memcpy(o, g[j], sizeof(g[j]));
-            } else {
-#pragma unroll
-                for (int k = 0; k < V; ++k)
-                    if (c + k < H) o[k] = g[j][k];
-            }
+            store_row_piece<float, V>(a.dx + row * H + c, H - c, g[j]);
         }
     }
     float *part = a.part + (int64_t)blockIdx.x * 2 * H;
@@ -383,7 +462,7 @@ extern "C" int jitdb_dropout(const void *x, int64_t n, jitdb_dtype dtype, float 
     const Drop d = make_drop(p, state);
     hipStream_t st = (hipStream_t)hip_stream;
     const int vec = dtype == JITDB_F32 ? kVec<float> : kVec<bf16_t>;
-    const int64_t want = ceil_div(n, (int64_t)kT * vec);
+    const int64_t want = ceil_div(n, (int64_t)kT * vec * 4);
     const unsigned blocks = (unsigned)(want < 4096 ? want : 4096);
     if (dtype == JITDB_F32) dropout_kernel<float><<<blocks, kT, 0, st>>>(static_cast<const float *>(x), n, d, static_cast<float *>(y));
     else dropout_kernel<bf16_t><<<blocks, kT, 0, st>>>(static_cast<const bf16_t *>(x), n, d, static_cast<bf16_t *>(y));
