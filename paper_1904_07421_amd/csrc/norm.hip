@@ -25,6 +25,7 @@ constexpr int kT = 256;
 constexpr int kWide = 512;               // threads that share a row of more than kWaveMax values
 constexpr int kWaveMax = 2048;
 constexpr int kMaxWidth = 1 << 14;
+constexpr int kForwardBlocks = 8192;     // of the forward pass (2048 take 10 to 15 % longer on a million rows)
 constexpr int kMaxParts = 1024;          // partial sums of the weight gradients: blocks of the backward pass
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
@@ -122,11 +123,12 @@ __device__ __forceinline__ void store_row_piece(T *p, int left, const float (&v)
         else e[k] = __builtin_bit_cast(bf16_t, (__bf16)v[k]);          // (the hardware's rounding, two a instruction)
     }
     if (left >= N) {
-#pragma unroll
-        for (int q = 0; q < N / kVec<T>; ++q) {
+        if constexpr (N == kVec<T>) {
             u32x4 w;
-            __builtin_memcpy(&w, e + q * kVec<T>, 16);
-            __builtin_nontemporal_store(w, reinterpret_cast<any4 *>(p + q * kVec<T>));
+            __builtin_memcpy(&w, e, 16);
+            __builtin_nontemporal_store(w, reinterpret_cast<any4 *>(p));
+        } else {                         // (in two halves or quarters: the caches make whole lines of them; past them, dx takes 16 % longer)
+            __builtin_memcpy(p, e, sizeof(e));
         }
     } else {
 #pragma unroll
@@ -400,7 +402,7 @@ int norm_groups(int H, int vec) {       // rows that a block works on at once
     const int pieces = (int)ceil_div(H, vec);
     return H > kWaveMax ? 1 : pieces <= 16 ? kT / 16 : pieces <= 32 ? kT / 32 : kT / 64;
 }
-// 8 blocks a CU, fewer where there are fewer rows
+// no more blocks than there are rows for
 int norm_blocks(int64_t n, int H, int vec, int most) {
     const int64_t b = ceil_div(n, norm_groups(H, vec));
     return (int)(b < most ? b : most);
@@ -421,7 +423,7 @@ void for_width(int H, F &&launch) {
 
 template <typename T>
 int run_forward_norm(const NormArgs &a, hipStream_t st) {
-    const int blocks = norm_blocks(a.n, a.H, kVec<T>, 2048);
+    const int blocks = norm_blocks(a.n, a.H, kVec<T>, kForwardBlocks);
     for_width<kVec<T>>(a.H, [&](auto g, auto nv) {
         constexpr int G = decltype(g)::value, NV = decltype(nv)::value;
         layernorm_kernel<T, G, NV><<<blocks, G <= 64 ? kT : kWide, 0, st>>>(a);
