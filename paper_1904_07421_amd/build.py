@@ -7,6 +7,7 @@ import shutil
 import subprocess
 import sys
 import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -221,14 +222,27 @@ def check_mfma_results(asm_text: str, kernel_substr: str = "kernel") -> int:
 _VMEM = re.compile(r"(global|buffer|flat|scratch)_(load|store|atomic)")
 
 
-def check_stage_loads(asm_text: str, kernel_substr: str = "level_kernel") -> int:
+def _mfma_loops(body) -> list:
+    """The innermost of a kernel's loops that hold MFMAs, each as its instructions."""
+    labels = {l[:-1]: i for i, l in enumerate(body) if l.endswith(":")}
+    loops = {}
+    for i, l in enumerate(body):
+        p = l.split()
+        if len(p) >= 2 and (p[0].startswith("s_cbranch") or p[0] == "s_branch") and p[1] in labels and labels[p[1]] <= i:
+            head = labels[p[1]]
+            loops[head] = max(loops.get(head, head), i)
+    with_mfma = [(a, b) for a, b in loops.items() if any(l.startswith("v_mfma") for l in body[a:b + 1])]
+    return [body[a:b + 1] for a, b in with_mfma if not any(a < a2 and b2 <= b for a2, b2 in with_mfma)]
+
+
+def check_stage_loads(asm_text: str, kernel_substr: str = "level_kernel", expected: int | None = None) -> int:
     """Static check of the K loops of the kernels that move pipeline stages with direct-to-LDS loads
     and wait for them with hand-written `s_waitcnt vmcnt(N)`: N is a number of loads of a YOUNGER
     stage that may stay in flight, so it is only right if every wave issues exactly the expected
     loads per stage and nothing else joins the same counter in between.  For every innermost loop
     that holds MFMAs, the only vector-memory instructions must be global_load_lds_dwordx4, and their
-    number must be (loads per wave and stage) x (barriers in the loop): 5 for the leaf level kernel
-    (its blocks skip the forget rows), 6 otherwise.  Returns the number of loops examined."""
+    number must be (loads per wave and stage) x (barriers in the loop): `expected`, or 5 for the leaf
+    level kernel (its blocks skip the forget rows) and 6 otherwise.  Returns the number of loops examined."""
     kernels, cur, name = [], None, None
     for raw in asm_text.splitlines():
         line = raw.split(";")[0].strip()
@@ -245,19 +259,8 @@ def check_stage_loads(asm_text: str, kernel_substr: str = "level_kernel") -> int
     examined = 0
     for name, body in kernels:
         m = re.search(r"level_kernelI[a-z]Li(\d)E", name)
-        per_stage = 5 if (m and m.group(1) == "0") else 6
-        labels = {l[:-1]: i for i, l in enumerate(body) if l.endswith(":")}
-        loops = {}
-        for i, l in enumerate(body):
-            p = l.split()
-            if len(p) >= 2 and (p[0].startswith("s_cbranch") or p[0] == "s_branch") and p[1] in labels and labels[p[1]] <= i:
-                head = labels[p[1]]
-                loops[head] = max(loops.get(head, head), i)
-        with_mfma = [(a, b) for a, b in loops.items() if any(l.startswith("v_mfma") for l in body[a:b + 1])]
-        for a, b in with_mfma:
-            if any(a < a2 and b2 <= b for a2, b2 in with_mfma):
-                continue                                   # not innermost
-            seg = body[a:b + 1]
+        per_stage = expected or (5 if (m and m.group(1) == "0") else 6)
+        for seg in _mfma_loops(body):
             other = [l for l in seg if _VMEM.match(l) and not l.startswith("global_load_lds_dwordx4")]
             if other:
                 raise RuntimeError(f"{name}: a K loop holds a vector-memory instruction besides the stage loads: {other[0]}")
@@ -272,26 +275,61 @@ def check_stage_loads(asm_text: str, kernel_substr: str = "level_kernel") -> int
     return examined
 
 
+def check_walk_loads(asm_text: str, kernel_substr: str) -> int:
+    """Static check of the loops that walk over tiles of a streaming operand, one barrier a tile, and keep one younger tile's
+    direct-to-LDS loads in flight across it: the count that a barrier's wait leaves must be the number of such loads between
+    two barriers, and no other load may join the counter.  (Stores may: they only make the wait longer.)  Returns the number
+    of loops examined."""
+    examined = 0
+    for body in _kernel_bodies(asm_text, kernel_substr):
+        for seg in _mfma_loops(body):
+            other = [l for l in seg if re.match(r"(global|buffer|flat|scratch)_(load|atomic)", l) and not l.startswith("global_load_lds_")]
+            if other:
+                raise RuntimeError(f"{kernel_substr}: a walk holds a load besides the tiles': {other[0]}")
+            n_dma = sum(1 for l in seg if l.startswith("global_load_lds_"))
+            bars = [i for i, l in enumerate(seg) if l.startswith("s_barrier")]
+            waits = [re.match(r"s_waitcnt vmcnt\((\d+)\)", seg[i - 1]) for i in bars]
+            if not bars or any(w is None or int(w.group(1)) * len(bars) != n_dma for w in waits):
+                raise RuntimeError(f"{kernel_substr}: a walk issues {n_dma} loads for {len(bars)} barrier(s), whose waits leave "
+                                   f"{[w and w.group(1) for w in waits]} in flight")
+            examined += 1
+    return examined
+
+
 def build(verbose: bool = False) -> str:
     """Always recompiles every source; returns the path of the shared library."""
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     srcs = [os.path.join(CSRC, s) for s in SOURCES if os.path.exists(os.path.join(CSRC, s))]
-    cmd = [hipcc, *HIPCC_FLAGS, "--save-temps", "-I", os.path.join(ROOT, "include"), "-I", CSRC, "-o", LIB, *srcs]
-    if verbose:
-        print(" ".join(cmd), flush=True)
+    compile_flags = [f for f in HIPCC_FLAGS if f != "-shared"] + ["--save-temps", "-I", os.path.join(ROOT, "include"), "-I", CSRC]
     tmp = tempfile.mkdtemp(prefix="jitdb_build_")
+
+    def run(cmd, cwd):
+        if verbose:
+            print(" ".join(cmd), flush=True)
+        return subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True, cwd=cwd)
+
+    def compile_one(src):
+        stem = os.path.splitext(os.path.basename(src))[0]
+        own = os.path.join(tmp, stem)
+        os.mkdir(own)
+        return run([hipcc, *compile_flags, "-c", "-o", os.path.join(tmp, stem + ".o"), src], own)
+
     try:
-        res = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True, cwd=tmp)
+        with ThreadPoolExecutor(max_workers=min(8, os.cpu_count() or 1)) as pool:
+            results = list(pool.map(compile_one, srcs))
+        if all(r.returncode == 0 for r in results):
+            objects = [os.path.join(tmp, os.path.splitext(os.path.basename(src))[0] + ".o") for src in srcs]
+            results.append(run([hipcc, "--offload-arch=gfx950", "-fPIC", "-shared", "-o", LIB, *objects], tmp))
         asm_texts = {}
         for stem in ("forward", "backward", "trees", "xent", "probe"):
-            asm_path = os.path.join(tmp, stem + "-hip-amdgcn-amd-amdhsa-gfx950.s")
+            asm_path = os.path.join(tmp, stem, stem + "-hip-amdgcn-amd-amdhsa-gfx950.s")
             asm_texts[stem] = open(asm_path).read() if os.path.exists(asm_path) else None
     finally:
         shutil.rmtree(tmp, ignore_errors=True)
     # the host pass warns that it does not know the packed-fp32 feature: harmless
-    lines = [l for l in res.stdout.splitlines() if "packed-fp32-ops" not in l]
+    lines = [l for r in results for l in r.stdout.splitlines() if "packed-fp32-ops" not in l]
     out = "\n".join(l for l in lines if "-Rpass-analysis" not in l)
-    if res.returncode != 0:
+    if any(r.returncode != 0 for r in results):
         raise RuntimeError("hipcc failed:\n" + out)
     _check_no_scratch(lines)
     for stem, text in asm_texts.items():
@@ -303,15 +341,18 @@ def build(verbose: bool = False) -> str:
     # (names with their length prefix, as they are mangled: "level_kernel" alone would also match fused_level_kernel)
     for stem, name in (("forward", "12level_kernel"), ("forward", "14gemm_kb_kernel"), ("forward", "17nary_level_kernel"),
                        ("backward", "16rows_tile_kernel"), ("backward", "9tn_kernel"),
-                       ("xent", "13logits_kernel"), ("xent", "19grad_product_kernel")):
+                       ("xent", "19grad_product_kernel"), ("xent", "18wide_logits_kernel"), ("xent", "15resident_kernel")):
         if check_lds_read_waits(asm_texts[stem], name) == 0:
             raise RuntimeError(f"no LDS reads found in the assembly of {name}: the check is not looking at it")
     # the K loops whose waits for direct-to-LDS stage loads are hand-counted
-    for stem, name in (("forward", "12level_kernel"), ("forward", "14gemm_kb_kernel"), ("forward", "17nary_level_kernel"),
-                       ("backward", "16rows_tile_kernel"), ("backward", "9tn_kernel"),
-                       ("xent", "13logits_kernel"), ("xent", "19grad_product_kernel")):
-        if check_stage_loads(asm_texts[stem], name) == 0:
+    for stem, name, expected in (("forward", "12level_kernel", None), ("forward", "14gemm_kb_kernel", None),
+                                 ("forward", "17nary_level_kernel", None), ("backward", "16rows_tile_kernel", None),
+                                 ("backward", "9tn_kernel", None), ("xent", "19grad_product_kernelILi4E", 4),
+                                 ("xent", "19grad_product_kernelILi2E", 6), ("xent", "18wide_logits_kernel", 6)):
+        if check_stage_loads(asm_texts[stem], name, expected) == 0:
             raise RuntimeError(f"no K loop with stage loads found in the assembly of {name}: the check is not looking at it")
+    if check_walk_loads(asm_texts["xent"], "15resident_kernel") == 0:
+        raise RuntimeError("no walk found in the assembly of resident_kernel: the check is not looking at it")
     if verbose and out.strip():
         print(out)
     return LIB

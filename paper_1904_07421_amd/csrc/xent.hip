@@ -23,10 +23,9 @@
 namespace jitdb {
 namespace {
 
-constexpr int kT = 256;
 constexpr int kMaxClasses = 1 << 22;
 constexpr int kMaxWidth = 1 << 14;
-constexpr int kLabelBlock = 4096;             // labels of a block of the two listing kernels
+constexpr int kLabelBlock = 1024, kLabelBlocks = 2048;     // labels of a block of the listing kernels at least, most blocks of them
 constexpr int64_t kStatBytes = 512ll << 20;   // of tile statistics of wide states kept at once (forward) ...
 constexpr int64_t kGradBytes = 4ll << 30;     // ... and of g (backward): rows beyond come in further chunks
 
@@ -35,7 +34,7 @@ struct RowList {
     const int32_t *label;       // [N], -1: none
     const float *lse, *gloss;   // [N] (backward); gloss may be nullptr
     int64_t n;
-    int C;
+    int C, per_block;           // labels of a block
     float lse_scale;            // of the records' log-sum-exp
     int32_t *counts;            // labelled rows of each block of labels
     int32_t *n_rows;            // how many there are
@@ -44,17 +43,16 @@ struct RowList {
     float *side;                // backward: records of 32 rows, as in ResArgs
     float *loss_out, *lse_out;  // forward: 0 for rows without a label
 };
-__global__ void __launch_bounds__(kT)
-label_count_kernel(const RowList a) {
+__device__ __forceinline__ void count_labels(const RowList &a, int block) {
     __shared__ int32_t red[kT / 64];
     int c = 0;
-    const int64_t at = (int64_t)blockIdx.x * kLabelBlock;
-    for (int i = threadIdx.x; i < kLabelBlock; i += kT) c += at + i < a.n && a.label[at + i] != -1;
+    const int64_t at = (int64_t)block * a.per_block;
+    for (int i = threadIdx.x; i < a.per_block; i += kT) c += at + i < a.n && a.label[at + i] != -1;
 #pragma unroll
     for (int m = 1; m < 64; m <<= 1) c += __shfl_xor(c, m);
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = c;
     __syncthreads();
-    if (threadIdx.x == 0) a.counts[blockIdx.x] = red[0] + red[1] + red[2] + red[3];
+    if (threadIdx.x == 0) a.counts[block] = red[0] + red[1] + red[2] + red[3];
 }
 // Lists the rows in ascending order.  The last block also knows their number, and fills the last 256 rows' records.
 __global__ void __launch_bounds__(kT)
@@ -74,8 +72,8 @@ label_rows_kernel(const RowList a) {
         rec[32] = w;
         rec[64] = __int_as_float(label);
     };
-    for (int i0 = 0; i0 < kLabelBlock; i0 += kT) {
-        const int64_t i = (int64_t)blockIdx.x * kLabelBlock + i0 + t;
+    for (int i0 = 0; i0 < a.per_block; i0 += kT) {
+        const int64_t i = (int64_t)blockIdx.x * a.per_block + i0 + t;
         const int32_t label = i < a.n ? a.label[i] : -1;
         const bool has = label != -1;
         const uint64_t votes = __ballot(has);
@@ -123,16 +121,14 @@ __device__ __forceinline__ void store_parts(const T (&e)[8], char *to, int64_t p
         }
     }
 }
-// Eight elements a thread; rows past the last one up to a multiple of `pad` are zero.  map: row r of the operand is row map[r] of src.
+// Eight elements a thread; rows past the last one up to a multiple of 256 are zero.  map: row r of the operand is row map[r] of src.
 template <typename T, int PARTS>
-__global__ void __launch_bounds__(kT)
-pack_rows_kernel(const T *__restrict__ src, const int32_t *__restrict__ map, const int32_t *__restrict__ n_dev, int64_t n_host, int width,
-                 int slabs, int pad, Operand o) {
-    const int64_t n = n_dev ? *n_dev : n_host, rows = (n + pad - 1) / pad * pad;
-    const int pieces = slabs * 4;
-    const int64_t total = rows * pieces;
-    for (int64_t q = (int64_t)blockIdx.x * kT + threadIdx.x; q < total; q += (int64_t)gridDim.x * kT) {
-        const int64_t r = q / pieces;
+__device__ __forceinline__ void pack_rows(const T *__restrict__ src, const int32_t *__restrict__ map, int64_t n, int width, int slabs,
+                                          const Operand &o, int block, int n_blocks) {
+    const uint32_t pieces = (uint32_t)slabs * 4;
+    const int64_t total = (n + 255) / 256 * 256 * pieces;
+    for (int64_t q = (int64_t)block * kT + threadIdx.x; q < total; q += (int64_t)n_blocks * kT) {
+        const int64_t r = total >> 32 ? q / pieces : (int64_t)((uint32_t)q / pieces);
         const int piece = (int)(q - r * pieces), k = piece * 8;
         T e[8];
 #pragma unroll
@@ -150,47 +146,93 @@ pack_rows_kernel(const T *__restrict__ src, const int32_t *__restrict__ map, con
         store_parts<T, PARTS>(e, o.at + (piece >> 2) * o.slab + r * 64 + (piece & 3) * 16, o.part);
     }
 }
-// The turned states: row f = feature (f_rows of them, zero behind the last), K = row of the list, up to a multiple of 64.  Blocks of
-// 32 rows x 64 features turn through LDS.
+// The turned states: row f = feature (f_rows of them, zero behind the last), K = row of the list, up to a multiple of 64.  A block
+// turns 32 rows x 64 features through LDS.
 template <typename T, int PARTS>
-__global__ void __launch_bounds__(kT)
-pack_turned_kernel(const T *__restrict__ src, const int32_t *__restrict__ map, const int32_t *__restrict__ n_dev, int H, int f_rows, Operand o) {
+__device__ __forceinline__ void pack_turned(const T *__restrict__ src, const int32_t *__restrict__ map, int n, int H, int f_rows, const Operand &o,
+                                            int block, int n_blocks) {
     __shared__ T tile[32][65];
-    const int n = *n_dev, r0 = blockIdx.x * 32, f0 = blockIdx.y * 64, t = threadIdx.x;
-    if (r0 >= (n + 63) / 64 * 64) return;
-    for (int i = t >> 6; i < 32; i += 4) {
-        const int f = f0 + (t & 63);
-        tile[i][t & 63] = r0 + i < n && f < H ? src[(int64_t)map[r0 + i] * H + f] : T(0);
-    }
-    __syncthreads();
-    const int f = t >> 2, piece = t & 3;
-    if (f0 + f >= f_rows) return;
-    T e[8];
+    const int t = threadIdx.x, f_blocks = f_rows / 64, r_blocks = (n + 63) / 64 * 2;
+    for (int64_t q = block; q < (int64_t)f_blocks * r_blocks; q += n_blocks) {
+        const int rb = (int)(q / f_blocks), r0 = rb * 32, f0 = (int)(q - (int64_t)rb * f_blocks) * 64;
+        for (int i = t >> 6; i < 32; i += 4) {
+            const int f = f0 + (t & 63);
+            tile[i][t & 63] = r0 + i < n && f < H ? src[(int64_t)map[r0 + i] * H + f] : T(0);
+        }
+        __syncthreads();
+        const int f = t >> 2, piece = t & 3;
+        T e[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) e[j] = tile[piece * 8 + j][f];
-    store_parts<T, PARTS>(e, o.at + blockIdx.x * o.slab + (int64_t)(f0 + f) * 64 + piece * 16, o.part);
-}
-__global__ void __launch_bounds__(kT)
-pad_bias_kernel(const float *__restrict__ b, int C, int n, float *__restrict__ out) {
-    for (int c = blockIdx.x * kT + threadIdx.x; c < n; c += gridDim.x * kT) out[c] = c >= C ? -INFINITY : b ? b[c] : 0.0f;
+        for (int j = 0; j < 8; ++j) e[j] = tile[piece * 8 + j][f];
+        store_parts<T, PARTS>(e, o.at + rb * o.slab + (int64_t)(f0 + f) * 64 + piece * 16, o.part);
+        __syncthreads();
+    }
 }
 
 // z of the label itself, in fp32: a wave a row
 template <typename T>
-__global__ void __launch_bounds__(kT)
-label_logit_kernel(const T *__restrict__ h, const T *__restrict__ V, const float *__restrict__ b, const int32_t *__restrict__ n_rows,
-                   const int32_t *__restrict__ row_of, const int32_t *__restrict__ label_of, int H, float *__restrict__ out) {
+__device__ __forceinline__ void label_logits(const T *__restrict__ h, const T *__restrict__ V, const float *__restrict__ b, int n,
+                                             const int32_t *__restrict__ row_of, const int32_t *__restrict__ label_of, int H, float *__restrict__ out,
+                                             int block, int n_blocks) {
     const int lane = threadIdx.x & 63;
-    for (int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); r < *n_rows; r += (int64_t)gridDim.x * 4) {
+    for (int64_t r = (int64_t)block * 4 + (threadIdx.x >> 6); r < n; r += (int64_t)n_blocks * 4) {
         const int c = label_of[r];
         float s = 0.0f;
         if (c >= 0) {
             const T *x = h + (int64_t)row_of[r] * H, *v = V + (int64_t)c * H;
+#pragma unroll 4
             for (int k = lane; k < H; k += 64) s = fmaf(to_f32<T>(x[k]), to_f32<T>(v[k]), s);
         }
 #pragma unroll
         for (int m = 1; m < 64; m <<= 1) s += __shfl_xor(s, m);
         if (lane == 0) out[r] = c >= 0 ? s + (b ? b[c] : 0.0f) : __builtin_nanf("");
+    }
+}
+// rows without a label have no gradient
+template <typename O>
+__device__ __forceinline__ void clear_rows(const int32_t *__restrict__ label, int64_t n, int H, O *__restrict__ dh, int block, int n_blocks) {
+    const int lane = threadIdx.x & 63;
+    for (int64_t r = (int64_t)block * 4 + (threadIdx.x >> 6); r < n; r += (int64_t)n_blocks * 4)
+        if (label[r] == -1)
+            for (int k = lane; k < H; k += 64) dh[r * H + k] = O(0);
+}
+
+// ---- the two launches around the listing of the rows: work that does not depend on one another shares each
+struct PrepArgs {
+    RowList list;
+    const void *h, *V;
+    const float *b;
+    int H, C, Hf, slabs, n_bias;
+    Operand h_op, v_op, ht;
+    float *bias, *label_z;
+    void *dh;
+    int blocks[3];              // of each piece of work
+};
+// Counts the labels, packs the class weights, pads the bias.
+template <typename T, int PARTS>
+__global__ void __launch_bounds__(kT)
+before_rows_kernel(const PrepArgs a) {
+    int b = blockIdx.x;
+    if (b < a.blocks[0]) { count_labels(a.list, b); return; }
+    b -= a.blocks[0];
+    if (b < a.blocks[1]) { pack_rows<T, PARTS>(static_cast<const T *>(a.V), nullptr, a.C, a.H, a.slabs, a.v_op, b, a.blocks[1]); return; }
+    b -= a.blocks[1];
+    for (int c = b * kT + threadIdx.x; c < a.n_bias; c += a.blocks[2] * kT) a.bias[c] = c >= a.C ? -INFINITY : a.b ? a.b[c] : 0.0f;
+}
+// Packs the rows' states; forward: the labels' own logits; backward: the turned states, zeros for the rows without a label.
+template <typename T, int PARTS, bool BACKWARD, typename O>
+__global__ void __launch_bounds__(kT)
+after_rows_kernel(const PrepArgs a) {
+    int b = blockIdx.x;
+    const int n = *a.list.n_rows;
+    if (b < a.blocks[0]) { pack_rows<T, PARTS>(static_cast<const T *>(a.h), a.list.row_of, n, a.H, a.slabs, a.h_op, b, a.blocks[0]); return; }
+    b -= a.blocks[0];
+    if constexpr (!BACKWARD) {
+        label_logits<T>(static_cast<const T *>(a.h), static_cast<const T *>(a.V), a.b, n, a.list.row_of, a.list.label_of, a.H, a.label_z, b, a.blocks[1]);
+    } else {
+        if (b < a.blocks[1]) { pack_turned<T, PARTS>(static_cast<const T *>(a.h), a.list.row_of, n, a.H, a.Hf, a.ht, b, a.blocks[1]); return; }
+        b -= a.blocks[1];
+        clear_rows<O>(a.list.label, a.list.n, a.H, static_cast<O *>(a.dh), b, a.blocks[2]);
     }
 }
 
@@ -229,34 +271,6 @@ join_kernel(const float2 *__restrict__ stat, int n_stat, int class_tiles, int pl
     loss[at] = v - label_z[row0 + r];
 }
 
-// 64 classes a block; sixteen waves take every sixteenth of the sums there are (4 of each 256 rows, or, places > 0, one of each range of
-// resident_kernel's) in order
-__global__ void __launch_bounds__(1024)
-bias_grad_kernel(const float *__restrict__ part, int n_classes_pad, int places, int C, const int32_t *__restrict__ n_rows, int row0, int max_rows,
-                 int first, float *__restrict__ db) {
-    __shared__ float sums[16][64];
-    const int rows = chunk_rows(n_rows, row0, max_rows);
-    const int n = rows == 0 ? 0 : places > 0 ? res_ranges(n_classes_pad / kResRows, (rows + 63) / 64 * 2, places) : (rows + 255) / 256 * 4;
-    const int l = threadIdx.x & 63, q = threadIdx.x >> 6, c = blockIdx.x * 64 + l;
-    float s = 0.0f;
-    if (c < C)
-#pragma unroll 4
-        for (int p = q; p < n; p += 16) s += part[(int64_t)p * n_classes_pad + c];
-    sums[q][l] = s;
-    __syncthreads();
-    if (q || c >= C) return;
-    for (int k = 1; k < 16; ++k) s += sums[k][l];
-    db[c] = first ? s : db[c] + s;
-}
-// rows without a label have no gradient
-template <typename O>
-__global__ void __launch_bounds__(kT)
-clear_rows_kernel(const int32_t *__restrict__ label, int64_t n, int H, O *__restrict__ dh) {
-    const int lane = threadIdx.x & 63;
-    for (int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); r < n; r += (int64_t)gridDim.x * 4)
-        if (label[r] == -1)
-            for (int k = lane; k < H; k += 64) dh[r * H + k] = O(0);
-}
 template <typename O>
 __global__ void __launch_bounds__(kT)
 clear_kernel(O *__restrict__ p, int64_t n) {
@@ -269,7 +283,7 @@ struct Sizes {
     int H, C, Hk, Hf, Cp;      // widths: of K (states), of the turned states' rows, classes in whole tiles
     int at;                    // features of a tile of the gradients' products / 64
     int parts, g_parts;        // of the operands, of g
-    int label_blocks;
+    int label_per, label_blocks;
     int res, class_tiles;      // resident_kernel: K in steps of 16 (0: not for this width), tiles of 32 classes
     int stat_rows, grad_rows;  // rows of a chunk
 };
@@ -292,7 +306,8 @@ bool make_sizes(int64_t n, int32_t H, int32_t C, jitdb_dtype dtype, jitdb_dtype 
     s.class_tiles = (int)ceil_div(C, kResTile);
     s.parts = dtype == JITDB_F32 ? 3 : 1;
     s.g_parts = grad == JITDB_F32 ? 3 : 1;
-    s.label_blocks = (int)ceil_div(n > 0 ? n : 1, kLabelBlock);
+    s.label_per = kLabelBlock * (int)ceil_div(n > 0 ? n : 1, (int64_t)kLabelBlock * kLabelBlocks);
+    s.label_blocks = (int)ceil_div(n > 0 ? n : 1, s.label_per);
     auto chunk = [&](int64_t bytes_a_row, int64_t budget) {
         const int64_t rows = budget / bytes_a_row / 256 * 256;
         return (int)(rows < 256 ? 256 : rows < s.n_pad ? rows : s.n_pad);
@@ -360,18 +375,25 @@ unsigned grid_of(int64_t work) {        // grid of a kernel that loops: enough b
 }
 unsigned xcd_grid(int64_t blocks) { return (unsigned)(8 * ceil_div(blocks, 8)); }
 
-template <typename T>
-int prepare(const T *h, const T *V, const float *b, const RowList &list, const Sizes &s, const Space &w, hipStream_t st) {
+template <typename T, bool BACKWARD, typename O>
+int prepare(const T *h, const T *V, const float *b, const RowList &list, const Sizes &s, const Space &w, O *dh, hipStream_t st) {
     constexpr int PARTS = sizeof(T) == 4 ? 3 : 1;
-    label_count_kernel<<<s.label_blocks, kT, 0, st>>>(list);
+    PrepArgs a = {};
+    a.list = list; a.list.per_block = s.label_per;
+    a.h = h; a.V = V; a.b = b; a.H = s.H; a.C = s.C; a.Hf = s.Hf; a.slabs = s.Hk / 32; a.n_bias = s.Cp + 64;
+    a.h_op = w.h; a.v_op = w.v; a.ht = w.ht; a.bias = w.bias; a.label_z = w.label_z; a.dh = dh;
+    a.blocks[0] = s.label_blocks > 1 ? s.label_blocks : 0;          // (nobody asks a single block how many stand in front of it)
+    a.blocks[1] = (int)grid_of((int64_t)s.Cp * (s.Hk / 8));
+    a.blocks[2] = (int)(ceil_div(a.n_bias, kT) < 64 ? ceil_div(a.n_bias, kT) : 64);
+    before_rows_kernel<T, PARTS><<<(unsigned)(a.blocks[0] + a.blocks[1] + a.blocks[2]), kT, 0, st>>>(a);
     JITDB_LAUNCH_CHECK();
-    label_rows_kernel<<<s.label_blocks, kT, 0, st>>>(list);
+    label_rows_kernel<<<(unsigned)s.label_blocks, kT, 0, st>>>(a.list);
     JITDB_LAUNCH_CHECK();
-    pack_rows_kernel<T, PARTS><<<grid_of(s.n_pad * (s.Hk / 8)), kT, 0, st>>>(h, w.row_of, w.n_rows, 0, s.H, s.Hk / 32, 256, w.h);
-    JITDB_LAUNCH_CHECK();
-    pack_rows_kernel<T, PARTS><<<grid_of((int64_t)s.Cp * (s.Hk / 8)), kT, 0, st>>>(V, nullptr, nullptr, s.C, s.H, s.Hk / 32, 256, w.v);
-    JITDB_LAUNCH_CHECK();
-    pad_bias_kernel<<<grid_of(s.Cp + 64), kT, 0, st>>>(b, s.C, s.Cp + 64, w.bias);
+    a.blocks[0] = (int)grid_of(s.n_pad * (s.Hk / 8));
+    const int64_t waves = ceil_div(s.n, 4), turned = s.n_pad / 32 * (s.Hf / 64);
+    a.blocks[1] = (int)(BACKWARD ? (turned < 4096 ? turned : 4096) : (waves < 4096 ? waves : 4096));
+    a.blocks[2] = BACKWARD ? (int)(waves < 2048 ? waves : 2048) : 0;
+    after_rows_kernel<T, PARTS, BACKWARD, O><<<(unsigned)(a.blocks[0] + a.blocks[1] + a.blocks[2]), kT, 0, st>>>(a);
     JITDB_LAUNCH_CHECK();
     return JITDB_OK;
 }
@@ -394,11 +416,8 @@ int launch_resident(int steps, int64_t blocks, const ResArgs &a, hipStream_t st)
 template <typename T>
 int run_forward_xent(const T *h, const T *V, const float *b, const RowList &list, const Sizes &s, const Space &w,
                      float *loss, float *lse, hipStream_t st) {
-    int rc = prepare<T>(h, V, b, list, s, w, st);
+    int rc = prepare<T, false, T>(h, V, b, list, s, w, nullptr, st);
     if (rc != JITDB_OK) return rc;
-    const int64_t label_blocks = ceil_div(s.n, 4);
-    label_logit_kernel<T><<<(unsigned)(label_blocks < 8192 ? label_blocks : 8192), kT, 0, st>>>(h, V, b, w.n_rows, w.row_of, w.label_of, s.H, w.label_z);
-    JITDB_LAUNCH_CHECK();
     if (s.res) {
         ResArgs a = {};
         a.res = w.h.at; a.res_slab = w.h.slab; a.str = w.v.at; a.str_slab = w.v.slab; a.side = w.bias;
@@ -424,18 +443,14 @@ int run_forward_xent(const T *h, const T *V, const float *b, const RowList &list
     return JITDB_OK;
 }
 
-// dh and dV of one chunk of rows
+// dh, dV and db of one chunk of rows
 template <int WM, typename O>
-int run_grad_products(const Sizes &s, int64_t row_tiles, const GradArgs &gh, const GradArgs &gv, hipStream_t st) {
-    const int64_t h_tiles = gh.a_tiles * row_tiles, v_tiles = gv.a_tiles * ceil_div(s.C, kTileB);
-    const unsigned grid = xcd_grid((int64_t)grad_ranges(kTilePlaces<WM>, gh.a_tiles) * gh.a_tiles);
-    grad_product_kernel<false, WM><<<grid, kTileT<WM>, 0, st>>>(gh);
+int run_grad_products(int64_t row_tiles, const GradArgs &gh, const GradArgs &gv, BiasArgs bias, hipStream_t st) {
+    const int64_t ranges = grad_ranges(kTilePlaces<WM>, gh.a_tiles), h_blocks = gh.a_tiles * row_tiles * 32, v_blocks = gv.a_tiles * ceil_div(gv.C, kTileB) * 32;
+    const unsigned half = xcd_grid(ranges * gh.a_tiles);
+    grad_product_kernel<WM><<<2 * half, kTileT<WM>, 0, st>>>(gh, gv, (int)half);
     JITDB_LAUNCH_CHECK();
-    grad_finish_kernel<false, WM, O><<<(unsigned)(h_tiles * 32), kTileT<WM>, 0, st>>>(gh);
-    JITDB_LAUNCH_CHECK();
-    grad_product_kernel<true, WM><<<grid, kTileT<WM>, 0, st>>>(gv);
-    JITDB_LAUNCH_CHECK();
-    grad_finish_kernel<true, WM, O><<<(unsigned)(v_tiles * 32), kTileT<WM>, 0, st>>>(gv);
+    grad_finish_kernel<WM, O><<<(unsigned)(h_blocks + v_blocks + ceil_div(gv.C, 64)), kTileT<WM>, 0, st>>>(gh, gv, bias, h_blocks, v_blocks);
     JITDB_LAUNCH_CHECK();
     return JITDB_OK;
 }
@@ -443,14 +458,9 @@ int run_grad_products(const Sizes &s, int64_t row_tiles, const GradArgs &gh, con
 template <typename T, typename O>
 int run_backward_xent(const T *h, const T *V, const float *b, const RowList &list, const Sizes &s, const Space &w,
                       O *dh, O *dV, float *db, hipStream_t st) {
-    constexpr int PARTS = sizeof(T) == 4 ? 3 : 1, G_PARTS = sizeof(O) == 4 ? 3 : 1;
-    int rc = prepare<T>(h, V, b, list, s, w, st);
+    constexpr int G_PARTS = sizeof(O) == 4 ? 3 : 1;
+    int rc = prepare<T, true, O>(h, V, b, list, s, w, dh, st);
     if (rc != JITDB_OK) return rc;
-    pack_turned_kernel<T, PARTS><<<dim3((unsigned)(s.n_pad / 32), (unsigned)(s.Hf / 64)), kT, 0, st>>>(h, w.row_of, w.n_rows, s.H, s.Hf, w.ht);
-    JITDB_LAUNCH_CHECK();
-    const int64_t clear_blocks = ceil_div(s.n, 4);
-    clear_rows_kernel<O><<<(unsigned)(clear_blocks < 4096 ? clear_blocks : 4096), kT, 0, st>>>(list.label, s.n, s.H, dh);
-    JITDB_LAUNCH_CHECK();
     ResArgs ra = {};
     ra.res = w.v.at; ra.res_slab = w.v.slab; ra.str_slab = w.h.slab; ra.n_rows = w.n_rows; ra.max_rows = s.grad_rows;
     ra.class_blocks = s.Cp / kResRows; ra.bias = w.bias; ra.g = w.g.at; ra.g_slab = w.g.slab; ra.g_part = w.g.part; ra.db_part = w.db_part;
@@ -478,10 +488,9 @@ int run_backward_xent(const T *h, const T *V, const float *b, const RowList &lis
             wide_logits_kernel<G_PARTS, G_PARTS == 3><<<xcd_grid(2 * row_tiles * a.b_tiles), kTileT<2>, 0, st>>>(a);
             JITDB_LAUNCH_CHECK();
         }
-        bias_grad_kernel<<<(unsigned)ceil_div(s.C, 64), 1024, 0, st>>>(w.db_part, s.Cp, s.res ? res_places(s.parts * s.res, true) : 0, s.C, w.n_rows, a.row0, a.max_rows, gv.first, db);
-        JITDB_LAUNCH_CHECK();
         gv.p.A.at = w.ht.at + r0 / 32 * w.ht.slab;
-        rc = s.at == 4 ? run_grad_products<4, O>(s, row_tiles, gh, gv, st) : run_grad_products<2, O>(s, row_tiles, gh, gv, st);
+        const BiasArgs bias = {w.db_part, db, s.Cp, s.res ? res_places(s.parts * s.res, true) : 0};
+        rc = s.at == 4 ? run_grad_products<4, O>(row_tiles, gh, gv, bias, st) : run_grad_products<2, O>(row_tiles, gh, gv, bias, st);
         if (rc != JITDB_OK) return rc;
     }
     return JITDB_OK;

@@ -214,10 +214,11 @@ resident_kernel(const ResArgs a) {
     // ---- what happens to a tile of logits, dealt out over the products
     // Statistics: sums of exp(z - ref).  The reference is the maximum of the tiles up to the last one that left the range of fp32
     // (the first does): only then is a maximum taken and the sum so far scaled.
-    float ref[2] = {-INFINITY, -INFINITY}, ref_l[2] = {0.0f, 0.0f}, sum[2] = {__builtin_nanf(""), __builtin_nanf("")}, kept[2] = {0.0f, 0.0f};
+    // (A tile's sum is added to the others' as a whole: one chain over all classes would lose more to rounding.)
+    float ref[2] = {-INFINITY, -INFINITY}, ref_l[2] = {-INFINITY, -INFINITY}, sum[2] = {0.0f, 0.0f}, kept[2] = {0.0f, 0.0f};
     float late[2] = {0.0f, 0.0f}, arg = 0.0f;            // an exponential is added when the tile's next is asked for
     // Derivatives
-    float colsum[2] = {0.0f, 0.0f};
+    float colsum[2] = {0.0f, 0.0f}, tile_sum[2] = {0.0f, 0.0f};      // of the tiles before, of this one (as for the statistics)
     uint32_t words[G > 0 ? G : 1][2][2];                 // [part][q & 1][pair]
     float d[4];
     const int own_class = rb * kResRows + wave * 64 + l32;
@@ -241,7 +242,7 @@ resident_kernel(const ResArgs a) {
     auto statistics_end = [&](floatx16 (&z)[2]) __attribute__((always_inline)) {
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            sum[j] += late[j];
+            sum[j] = kept[j] + (sum[j] + late[j]);
             late[j] = 0.0f;
         }
         // (behind the branch accumulators may be moved: the last products are through by then, which the compiler does not see to there)
@@ -261,8 +262,11 @@ resident_kernel(const ResArgs a) {
                 ref[j] = out ? from : ref[j];
                 ref_l[j] = ref[j] * kLog2e;
             }
-        kept[0] = sum[0];
-        kept[1] = sum[1];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            kept[j] = sum[j];
+            sum[j] = 0.0f;
+        }
     };
     // g of element v of resident tile j; after every second quad 16 bytes a lane go out, the wave's halves having exchanged quads
     auto derivatives = [&](auto s_tag, floatx16 (&z)[2], int tile) __attribute__((always_inline)) {
@@ -273,7 +277,12 @@ resident_kernel(const ResArgs a) {
             const float x = z[J][V], lse = __uint_as_float(lse_w[0][Q][V % 4]), w = __uint_as_float(lse_w[1][Q][V % 4]);
             const float p = CLOSE ? exp_close(x - lse) : __builtin_amdgcn_exp2f(fmaf(x, kLog2e, -lse));
             d[V % 4] = p * w;
-            colsum[J] += d[V % 4];
+            if constexpr (V == 0) {
+                colsum[J] += tile_sum[J];
+                tile_sum[J] = d[0];
+            } else {
+                tile_sum[J] += d[V % 4];
+            }
             if constexpr (V % 4 == 3) {
 #pragma unroll
                 for (int i = 0; i < G; ++i) {
@@ -318,8 +327,8 @@ resident_kernel(const ResArgs a) {
             if (mine && (which & 31) == l32) {
                 const float p = CLOSE ? exp_close(x - lse) : __builtin_amdgcn_exp2f(fmaf(x, kLog2e, -lse));
                 float y = (p - 1.0f) * w;
-                if (which < 32) colsum[0] -= w;
-                else colsum[1] -= w;
+                if (which < 32) tile_sum[0] -= w;
+                else tile_sum[1] -= w;
 #pragma unroll
                 for (int i = 0; i < G; ++i) {
                     const uint32_t b = pack_bf16(y, 0.0f);
@@ -449,14 +458,14 @@ resident_kernel(const ResArgs a) {
     if constexpr (G == 0) {
 #pragma unroll
         for (int j = 0; j < 2; ++j) {        // the two lanes of a row
-            const float ref2 = __shfl_xor(ref[j], 32), sum2 = __shfl_xor(sum[j], 32), m = fmaxf(ref[j], ref2);
-            const float s = sum[j] * expf(ref[j] - m) + sum2 * expf(ref2 - m);
+            const float ref2 = __shfl_xor(ref[j], 32), sum2 = __shfl_xor(kept[j], 32), m = fmaxf(ref[j], ref2);
+            const float s = kept[j] * expf(ref[j] - m) + sum2 * expf(ref2 - m);
             if (hf == 0) a.stat[((int64_t)range * blocks + rb) * kResRows + wave * 64 + j * 32 + l32] = make_float2(m, s);
         }
     } else {
 #pragma unroll
         for (int j = 0; j < 2; ++j) {        // ... of a class
-            const float s = colsum[j] + __shfl_xor(colsum[j], 32);
+            const float own = colsum[j] + tile_sum[j], s = own + __shfl_xor(own, 32);
             if (hf == 0) a.db_part[(int64_t)range * blocks * kResRows + own_class + j * 32] = s;
         }
     }

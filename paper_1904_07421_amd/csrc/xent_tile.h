@@ -15,6 +15,7 @@ namespace jitdb {
 namespace {
 
 constexpr int kTileB = 256;                           // rows of B in a tile
+constexpr int kT = 256;                               // threads of the small kernels
 constexpr int kMaxPairs = 6;
 template <int WM> constexpr int kTileA = 64 * WM;     // rows of A
 template <int WM> constexpr int kTileT = 128 * WM;    // threads
@@ -191,9 +192,9 @@ __device__ __forceinline__ void clear_tile(floatx16 (&acc)[2][4]) {
 }
 
 // Blocks are dealt round-robin to the 8 XCDs, each with an L2 of its own: XCD x takes the x-th eighth of the places in order.
-__device__ __forceinline__ int64_t xcd_order(int64_t total) {
-    const int64_t per = (total + 7) / 8, i = (int64_t)(blockIdx.x & 7) * per + (blockIdx.x >> 3);
-    return (blockIdx.x >> 3) < per && i < total ? i : -1;
+__device__ __forceinline__ int64_t xcd_order(int64_t total, int block) {
+    const int64_t per = (total + 7) / 8, i = (int64_t)(block & 7) * per + (block >> 3);
+    return (block >> 3) < per && i < total ? i : -1;
 }
 __device__ __forceinline__ int chunk_rows(const int32_t *n_rows, int row0, int max_rows) {
     const int left = *n_rows - row0;
@@ -241,11 +242,9 @@ __device__ __forceinline__ GradPlan grad_plan(const GradArgs &a) {
     return g;
 }
 template <bool WEIGHTS, int WM>
-__global__ void __launch_bounds__(kTileT<WM>, 4 / WM)
-grad_product_kernel(const GradArgs a) {
-    __shared__ __attribute__((aligned(1024))) char lds[kTileBufs<WM> * kTileBuf<WM>];
+__device__ __forceinline__ void grad_product(const GradArgs &a, char *lds, int block) {
     const GradPlan g = grad_plan<WEIGHTS, WM>(a);
-    const int64_t place = xcd_order((int64_t)g.ranges * a.a_tiles);
+    const int64_t place = xcd_order((int64_t)g.ranges * a.a_tiles, block);
     if (place < 0) return;
     const int64_t range = place / a.a_tiles;
     const int at = (int)(place - range * a.a_tiles);
@@ -269,12 +268,19 @@ grad_product_kernel(const GradArgs a) {
         s += n;
     }
 }
+// The first `half` blocks (a multiple of 8) compute dh, as many more dV: where one leaves places on the chip, the other takes them.
+template <int WM>
+__global__ void __launch_bounds__(kTileT<WM>, 4 / WM)
+grad_product_kernel(const GradArgs h, const GradArgs v, int half) {
+    __shared__ __attribute__((aligned(1024))) char lds[kTileBufs<WM> * kTileBuf<WM>];
+    if ((int)blockIdx.x < half) grad_product<false, WM>(h, lds, blockIdx.x);
+    else grad_product<true, WM>(v, lds, blockIdx.x - half);
+}
 // 32 blocks a tile
 template <bool WEIGHTS, int WM, typename O>
-__global__ void __launch_bounds__(kTileT<WM>)
-grad_finish_kernel(const GradArgs a) {
+__device__ __forceinline__ void grad_finish(const GradArgs &a, int64_t block) {
     const GradPlan g = grad_plan<WEIGHTS, WM>(a);
-    const int tile = blockIdx.x >> 5, rest = blockIdx.x & 31, t = threadIdx.x;
+    const int tile = (int)(block >> 5), rest = (int)(block & 31), t = threadIdx.x;
     const int at = tile % a.a_tiles, bt = tile / a.a_tiles;
     if (bt >= g.b_tiles) return;
     const int lane = t & 63, wave = t >> 6, i = rest >> 4, j = (rest >> 2) & 3, v = rest & 3;
@@ -312,6 +318,39 @@ grad_finish_kernel(const GradArgs a) {
     }
 }
 
+// db: 64 classes a block; its waves take the sums there are (4 of each 256 rows, or, places > 0, one of each range of resident_kernel's)
+// in turn, each in order
+struct BiasArgs {
+    const float *part;
+    float *db;
+    int width, places;              // classes in whole blocks; resident_kernel's places
+};
+template <int WAVES>
+__device__ __forceinline__ void bias_finish(const BiasArgs &b, const GradArgs &a, int block) {
+    __shared__ float sums[WAVES][64];
+    const int rows = chunk_rows(a.n_rows, a.row0, a.max_rows);
+    const int n = rows == 0 ? 0 : b.places > 0 ? res_ranges(b.width / kResRows, (rows + 63) / 64 * 2, b.places) : (rows + 255) / 256 * 4;
+    const int l = threadIdx.x & 63, q = threadIdx.x >> 6, c = block * 64 + l;
+    float s = 0.0f;
+    if (c < a.C)
+#pragma unroll 4
+        for (int p = q; p < n; p += WAVES) s += b.part[(int64_t)p * b.width + c];
+    sums[q][l] = s;
+    __syncthreads();
+    if (q || c >= a.C) return;
+#pragma unroll
+    for (int k = 1; k < WAVES; ++k) s += sums[k][l];
+    b.db[c] = a.first ? s : b.db[c] + s;
+}
+template <int WM, typename O>
+__global__ void __launch_bounds__(kTileT<WM>)
+grad_finish_kernel(const GradArgs h, const GradArgs v, const BiasArgs bias, int64_t h_blocks, int64_t v_blocks) {
+    const int64_t b = blockIdx.x;
+    if (b < h_blocks) grad_finish<false, WM, O>(h, b);
+    else if (b < h_blocks + v_blocks) grad_finish<true, WM, O>(v, b - h_blocks);
+    else bias_finish<2 * WM>(bias, v, (int)(b - h_blocks - v_blocks));
+}
+
 // ---- logits of wide states: both operands stream ---------------------------------------------------------
 // G = 0: A = class weights, B = states; statistics of every 64 classes.  G > 0: A = states, B = class weights; g.
 struct LogitArgs {
@@ -331,7 +370,7 @@ wide_logits_kernel(const LogitArgs a) {
     __shared__ __attribute__((aligned(1024))) char lds[kTileBufs<2> * kTileBuf<2>];
     const int rows = chunk_rows(a.n_rows, a.row0, a.max_rows);
     const int row_tiles = (rows + 255) / 256 * (G == 0 ? 1 : 2), class_tiles = G == 0 ? a.a_tiles : a.b_tiles;
-    const int64_t i = xcd_order((int64_t)row_tiles * class_tiles);
+    const int64_t i = xcd_order((int64_t)row_tiles * class_tiles, (int)blockIdx.x);
     if (i < 0) return;
     // bands of eight row tiles, class tiles one after another inside a band: the blocks of an XCD share them in its L2
     const int band = (int)(i / (8 * (int64_t)class_tiles)), rem = (int)(i - (int64_t)band * 8 * class_tiles);
