@@ -446,11 +446,11 @@ int run_forward_xent(const T *h, const T *V, const float *b, const RowList &list
 // dh, dV and db of one chunk of rows
 template <int WM, typename O>
 int run_grad_products(int64_t row_tiles, const GradArgs &gh, const GradArgs &gv, BiasArgs bias, hipStream_t st) {
-    const int64_t ranges = grad_ranges(kTilePlaces<WM>, gh.a_tiles), h_blocks = gh.a_tiles * row_tiles * 32, v_blocks = gv.a_tiles * ceil_div(gv.C, kTileB) * 32;
+    const int64_t ranges = grad_ranges(kTilePlaces<WM>, gh.a_tiles), pieces = gh.a_tiles * (row_tiles + ceil_div(gv.C, kTileB)) * 8 + ceil_div(gv.C, 64);
     const unsigned half = xcd_grid(ranges * gh.a_tiles);
     grad_product_kernel<WM><<<2 * half, kTileT<WM>, 0, st>>>(gh, gv, (int)half);
     JITDB_LAUNCH_CHECK();
-    grad_finish_kernel<WM, O><<<(unsigned)(h_blocks + v_blocks + ceil_div(gv.C, 64)), kTileT<WM>, 0, st>>>(gh, gv, bias, h_blocks, v_blocks);
+    grad_finish_kernel<WM, O><<<(unsigned)(pieces < 4096 ? pieces : 4096), kTileT<WM>, 0, st>>>(gh, gv, bias);
     JITDB_LAUNCH_CHECK();
     return JITDB_OK;
 }
@@ -477,7 +477,6 @@ int run_backward_xent(const T *h, const T *V, const float *b, const RowList &lis
     for (int64_t r0 = 0; r0 < s.n; r0 += s.grad_rows) {
         const int64_t rows = s.n - r0 < s.grad_rows ? s.n - r0 : s.grad_rows, row_tiles = ceil_div(rows, 256);
         ra.row0 = a.row0 = gh.row0 = gv.row0 = (int)r0;
-        gv.first = r0 == 0; gv.last = r0 + s.grad_rows >= s.n;
         if (s.res) {
             ra.str = w.h.at + r0 * 64;
             ra.side = w.side + r0 * 4;

@@ -218,13 +218,11 @@ struct GradArgs {
     int H;
     void *out;
     float *acc;                     // dV over several chunks of rows
-    int first, last;
 };
-constexpr int kMinStages = 8;       // a range is no shorter
+constexpr uint32_t kMinStages = 8;       // a range is no shorter
 struct GradPlan {
-    int b_tiles, nk, stages;        // stages of a part product, of a tile
-    int64_t total;
-    int per, ranges;
+    uint32_t b_tiles, nk, stages;   // stages of a part product, of a tile
+    uint32_t total, per, ranges;    // (a stage stands for 8192 elements of g, six times at most: of a chunk of rows far below 2^32)
 };
 __host__ __device__ inline int grad_ranges(int places, int a_tiles) { return places > a_tiles ? places / a_tiles : 1; }      // at most
 template <bool WEIGHTS, int WM>
@@ -234,11 +232,10 @@ __device__ __forceinline__ GradPlan grad_plan(const GradArgs &a) {
     g.b_tiles = WEIGHTS ? (a.C + kTileB - 1) / kTileB : (rows + kTileB - 1) / kTileB;
     g.nk = WEIGHTS ? (rows + 31) / 32 : (a.C + 31) / 32;
     g.stages = g.nk * a.p.pairs.n;
-    g.total = (int64_t)g.b_tiles * g.stages;
-    const int most = grad_ranges(kTilePlaces<WM>, a.a_tiles);
-    const int64_t per = (g.total + most - 1) / most;
-    g.per = (int)(per > kMinStages ? per : kMinStages);
-    g.ranges = (int)((g.total + g.per - 1) / g.per);
+    g.total = g.b_tiles * g.stages;
+    const uint32_t most = grad_ranges(kTilePlaces<WM>, a.a_tiles), per = (g.total + most - 1) / most;
+    g.per = per > kMinStages ? per : kMinStages;
+    g.ranges = (g.total + g.per - 1) / g.per;
     return g;
 }
 template <bool WEIGHTS, int WM>
@@ -246,18 +243,16 @@ __device__ __forceinline__ void grad_product(const GradArgs &a, char *lds, int b
     const GradPlan g = grad_plan<WEIGHTS, WM>(a);
     const int64_t place = xcd_order((int64_t)g.ranges * a.a_tiles, block);
     if (place < 0) return;
-    const int64_t range = place / a.a_tiles;
-    const int at = (int)(place - range * a.a_tiles);
-    int64_t s = range * g.per;
-    const int64_t end = s + g.per < g.total ? s + g.per : g.total;
+    const uint32_t range = (uint32_t)place / (uint32_t)a.a_tiles, at = (uint32_t)place - range * a.a_tiles;
+    uint32_t s = range * g.per;
+    const uint32_t end = s + g.per < g.total ? s + g.per : g.total;
     while (s < end) {
-        const int bt = (int)(s / g.stages), s0 = (int)(s - (int64_t)bt * g.stages);
-        const int n = end - s < g.stages - s0 ? (int)(end - s) : g.stages - s0;
+        const uint32_t bt = s / g.stages, s0 = s - bt * g.stages, n = end - s < g.stages - s0 ? end - s : g.stages - s0;
         floatx16 acc[2][4];
         clear_tile(acc);
         if constexpr (WEIGHTS) multiply_tile<false, WM>(a.p, (int64_t)at * kTileA<WM>, (int64_t)bt * kTileB, g.nk, s0, n, lds, acc);
-        else multiply_tile<true, WM>(a.p, at * (kTileA<WM> / 32), bt * (kTileB / 32), g.nk, s0, n, lds, acc);
-        float4 *out = reinterpret_cast<float4 *>(a.part + ((bt + range) * a.a_tiles + at) * (kTileA<WM> * kTileB)) + threadIdx.x;
+        else multiply_tile<true, WM>(a.p, (int64_t)at * (kTileA<WM> / 32), (int64_t)bt * (kTileB / 32), g.nk, s0, n, lds, acc);
+        float4 *out = reinterpret_cast<float4 *>(a.part + ((int64_t)(bt + range) * a.a_tiles + at) * (kTileA<WM> * kTileB)) + threadIdx.x;
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -276,45 +271,55 @@ grad_product_kernel(const GradArgs h, const GradArgs v, int half) {
     if ((int)blockIdx.x < half) grad_product<false, WM>(h, lds, blockIdx.x);
     else grad_product<true, WM>(v, lds, blockIdx.x - half);
 }
-// 32 blocks a tile
+// A tile's shares are put together in 8 pieces; a lane writes 32 features of its row or class, the wave's halves taking every other
+// four, so that what a block writes of a row is at least half a line (512 x 32000 bf16: 81 us; pieces of four features, whose lines several XCDs share: 127 us
+// in this loop).
 template <bool WEIGHTS, int WM, typename O>
-__device__ __forceinline__ void grad_finish(const GradArgs &a, int64_t block) {
-    const GradPlan g = grad_plan<WEIGHTS, WM>(a);
-    const int tile = (int)(block >> 5), rest = (int)(block & 31), t = threadIdx.x;
-    const int at = tile % a.a_tiles, bt = tile / a.a_tiles;
-    if (bt >= g.b_tiles) return;
-    const int lane = t & 63, wave = t >> 6, i = rest >> 4, j = (rest >> 2) & 3, v = rest & 3;
-    const int m = at * kTileA<WM> + (wave >> 1) * 64 + i * 32 + v * 8 + (lane >> 5) * 4;     // first of four features
+__device__ __forceinline__ void grad_finish(const GradArgs &a, const GradPlan &g, int64_t piece) {
+    const int i = (int)(piece >> 2) & 1, j = (int)piece & 3, t = threadIdx.x;
+    const uint32_t tile = (uint32_t)(piece >> 3), bt = tile / (uint32_t)a.a_tiles, at = tile - bt * a.a_tiles;
+    const int lane = t & 63, wave = t >> 6;
+    const int m0 = at * kTileA<WM> + (wave >> 1) * 64 + i * 32 + (lane >> 5) * 4;                // first feature, and 8, 16, 24 on
     const int n = bt * kTileB + (wave & 1) * 128 + j * 32 + (lane & 31);                          // row or class
-    if (m >= a.H || n >= (WEIGHTS ? a.C : chunk_rows(a.n_rows, a.row0, a.max_rows))) return;
-    float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (m0 >= a.H || n >= (WEIGHTS ? a.C : chunk_rows(a.n_rows, a.row0, a.max_rows))) return;
+    float s[4][4] = {};
     if (g.stages > 0) {
-        const int64_t first = (int64_t)bt * g.stages / g.per, last = ((int64_t)(bt + 1) * g.stages - 1) / g.per;
-        const float4 *in = reinterpret_cast<const float4 *>(a.part + ((bt + first) * a.a_tiles + at) * (kTileA<WM> * kTileB)) + rest * kTileT<WM> + t;
-#pragma unroll 4
-        for (int64_t k = first; k <= last; ++k) {
-            const float4 p = in[(k - first) * a.a_tiles * (kTileA<WM> * kTileB / 4)];
-            s[0] += p.x; s[1] += p.y; s[2] += p.z; s[3] += p.w;
+        const uint32_t first = bt * g.stages / g.per, last = ((bt + 1) * g.stages - 1) / g.per;
+        const float4 *in = reinterpret_cast<const float4 *>(a.part + ((int64_t)(bt + first) * a.a_tiles + at) * (kTileA<WM> * kTileB)) + (i * 4 + j) * 4 * kTileT<WM> + t;
+#pragma unroll 2
+        for (uint32_t k = first; k <= last; ++k) {
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+                const float4 p = in[v * kTileT<WM>];
+                s[v][0] += p.x; s[v][1] += p.y; s[v][2] += p.z; s[v][3] += p.w;
+            }
+            in += (int64_t)a.a_tiles * (kTileA<WM> * kTileB / 4);
         }
     }
-    const int64_t to = (WEIGHTS ? (int64_t)n : (int64_t)a.row_of[a.row0 + n]) * a.H + m;
-    const int left = a.H - m < 4 ? a.H - m : 4;
-    if (WEIGHTS && !a.first)
-        for (int k = 0; k < left; ++k) s[k] += a.acc[to + k];
-    if (WEIGHTS && !a.last) {
-        for (int k = 0; k < left; ++k) a.acc[to + k] = s[k];
-        return;
-    }
-    O e[4];
+    const int64_t row = (WEIGHTS ? (int64_t)n : (int64_t)a.row_of[a.row0 + n]) * a.H;
+    const bool more = WEIGHTS && *a.n_rows - a.row0 > a.max_rows;       // chunks to come
 #pragma unroll
-    for (int k = 0; k < 4; ++k) e[k] = from_f32<O>(s[k]);
-    O *o = static_cast<O *>(a.out) + to;
-    if (left == 4) {
-        __builtin_memcpy(o, e, sizeof(e));
-    } else {
+    for (int v = 0; v < 4; ++v) {
+        const int m = m0 + v * 8, left = a.H - m < 4 ? a.H - m : 4;
+        if (left <= 0) break;
+        const int64_t to = row + m;
+        if (WEIGHTS && a.row0 > 0)
+            for (int k = 0; k < left; ++k) s[v][k] += a.acc[to + k];
+        if (more) {
+            for (int k = 0; k < left; ++k) a.acc[to + k] = s[v][k];
+            continue;
+        }
+        O e[4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-            if (k < left) o[k] = e[k];
+        for (int k = 0; k < 4; ++k) e[k] = from_f32<O>(s[v][k]);
+        O *o = static_cast<O *>(a.out) + to;
+        if (left == 4) {
+            __builtin_memcpy(o, e, sizeof(e));
+        } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (k < left) o[k] = e[k];
+        }
     }
 }
 
@@ -326,29 +331,35 @@ struct BiasArgs {
     int width, places;              // classes in whole blocks; resident_kernel's places
 };
 template <int WAVES>
-__device__ __forceinline__ void bias_finish(const BiasArgs &b, const GradArgs &a, int block) {
-    __shared__ float sums[WAVES][64];
-    const int rows = chunk_rows(a.n_rows, a.row0, a.max_rows);
+__device__ __forceinline__ void bias_finish(const BiasArgs &b, const GradArgs &a, int rows, int c0, float (&sums)[WAVES][64]) {
     const int n = rows == 0 ? 0 : b.places > 0 ? res_ranges(b.width / kResRows, (rows + 63) / 64 * 2, b.places) : (rows + 255) / 256 * 4;
-    const int l = threadIdx.x & 63, q = threadIdx.x >> 6, c = block * 64 + l;
+    const int l = threadIdx.x & 63, q = threadIdx.x >> 6, c = c0 + l;
     float s = 0.0f;
     if (c < a.C)
 #pragma unroll 4
         for (int p = q; p < n; p += WAVES) s += b.part[(int64_t)p * b.width + c];
+    __syncthreads();                    // (the sums of the 64 classes before have been read)
     sums[q][l] = s;
     __syncthreads();
     if (q || c >= a.C) return;
 #pragma unroll
     for (int k = 1; k < WAVES; ++k) s += sums[k][l];
-    b.db[c] = a.first ? s : b.db[c] + s;
+    b.db[c] = a.row0 > 0 ? b.db[c] + s : s;
 }
+// Blocks take pieces in turn: how many there are depends on the number of rows, which the host does not know.
 template <int WM, typename O>
 __global__ void __launch_bounds__(kTileT<WM>)
-grad_finish_kernel(const GradArgs h, const GradArgs v, const BiasArgs bias, int64_t h_blocks, int64_t v_blocks) {
-    const int64_t b = blockIdx.x;
-    if (b < h_blocks) grad_finish<false, WM, O>(h, b);
-    else if (b < h_blocks + v_blocks) grad_finish<true, WM, O>(v, b - h_blocks);
-    else bias_finish<2 * WM>(bias, v, (int)(b - h_blocks - v_blocks));
+grad_finish_kernel(const GradArgs h, const GradArgs v, const BiasArgs bias) {
+    __shared__ float sums[2 * WM][64];
+    const int rows = chunk_rows(h.n_rows, h.row0, h.max_rows);
+    if (rows == 0 && h.row0 > 0) return;                         // the chunks before have had all rows
+    const GradPlan gh = grad_plan<false, WM>(h), gv = grad_plan<true, WM>(v);
+    const int64_t n_h = (int64_t)gh.b_tiles * h.a_tiles * 8, n_v = (int64_t)gv.b_tiles * v.a_tiles * 8, n = n_h + n_v + (v.C + 63) / 64;
+    for (int64_t i = blockIdx.x; i < n; i += gridDim.x) {
+        if (i < n_h) grad_finish<false, WM, O>(h, gh, i);
+        else if (i < n_h + n_v) grad_finish<true, WM, O>(v, gv, i - n_h);
+        else bias_finish<2 * WM>(bias, v, rows, (int)(i - n_h - n_v) * 64, sums);
+    }
 }
 
 // ---- logits of wide states: both operands stream ---------------------------------------------------------
