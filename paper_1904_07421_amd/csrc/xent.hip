@@ -501,7 +501,9 @@ bool few_fits(int H, int C, jitdb_dtype dtype) {
     auto any = [](auto, auto) {};
     return dtype == JITDB_F32 ? for_few<float>(H, C, any) : for_few<bf16_t>(H, C, any);
 }
-int few_blocks(int64_t n) {              // of the backward pass: each leaves a set of sums
+// Of the backward pass, each of which leaves a set of sums.  A single block writes the gradients itself, a launch less (62 rows of 160,
+// 5 classes, fp32: 12.1 -> 10.3 us in a graph; two turns of a single block lose: 128 rows 16.6 us, with two blocks 12.1).
+int few_blocks(int64_t n) {
     const int64_t b = ceil_div(n, kFewRows);
     return (int)(b < 1024 ? b : 1024);
 }
@@ -519,10 +521,12 @@ int run_few_forward(const FewArgs &a, hipStream_t st) {
     return JITDB_OK;
 }
 template <typename T, typename O>
-int run_few_backward(const FewArgs &a, O *dV, float *db, hipStream_t st) {
+int run_few_backward(FewArgs &a, O *dV, float *db, hipStream_t st) {
     const int blocks = few_blocks(a.n);
+    if (blocks == 1) { a.dV = dV; a.db = db; }
     for_few<T>(a.H, a.C, [&](auto c, auto nb) { few_backward_kernel<T, O, decltype(c)::value, decltype(nb)::value><<<blocks, kFewT, 0, st>>>(a); });
     JITDB_LAUNCH_CHECK();
+    if (blocks == 1) return JITDB_OK;
     few_reduce_kernel<O><<<(unsigned)ceil_div((int64_t)a.C * a.H + a.C, 64), 1024, 0, st>>>(a.part, blocks, a.H, a.C, dV, db);
     JITDB_LAUNCH_CHECK();
     return JITDB_OK;

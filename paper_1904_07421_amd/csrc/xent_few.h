@@ -31,6 +31,7 @@ struct FewArgs {
     const float *lse_in, *gloss;
     void *dh;
     float *part;                         // [blocks][C H + C]
+    void *dV; float *db;                 // of a single block
 };
 
 // The weights in LDS: in the order of the logits' loads, K in steps of four loads side by side.  Element e of piece (step s, quarter q)
@@ -280,6 +281,7 @@ few_backward_kernel(const FewArgs a) {
         }
     }
     float *part = a.part + (int64_t)blockIdx.x * ((int64_t)a.C * H + a.C);
+    O *own = static_cast<O *>(a.dV);                 // a single block's sums are the gradients
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
@@ -290,7 +292,10 @@ few_backward_kernel(const FewArgs a) {
                 if (c < a.C)
 #pragma unroll
                     for (int e = 0; e < V; ++e)
-                        if (f + e < H) part[(int64_t)c * H + f + e] = dv[nb][e][ct][v];
+                        if (f + e < H) {
+                            if (own) own[(int64_t)c * H + f + e] = from_f32<O>(dv[nb][e][ct][v]);
+                            else part[(int64_t)c * H + f + e] = dv[nb][e][ct][v];
+                        }
             }
     // the bias: over the 16 lanes that hold the same classes, then the four waves
     __syncthreads();
@@ -304,8 +309,9 @@ few_backward_kernel(const FewArgs a) {
             if (i16 == 0) gs[0][wave][ct * 16 + q * 4 + v] = s;
         }
     __syncthreads();
+    float *bias = own ? a.db : part + (int64_t)a.C * H;
     if ((int)threadIdx.x < a.C)
-        part[(int64_t)a.C * H + threadIdx.x] = gs[0][0][threadIdx.x] + gs[0][1][threadIdx.x] + gs[0][2][threadIdx.x] + gs[0][3][threadIdx.x];
+        bias[threadIdx.x] = gs[0][0][threadIdx.x] + gs[0][1][threadIdx.x] + gs[0][2][threadIdx.x] + gs[0][3][threadIdx.x];
 }
 
 // Value c of [n_parts][C H + C]: 64 values a block, sixteen waves take every sixteenth part in order, then the sixteen in order.
