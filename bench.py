@@ -46,7 +46,8 @@ def measured_traffic(cfg, key):
 
 def train_bench(args, J, torch, cfg, dev, N, D, H, esz, peak_tflops, xt, Wt, Ut, bt, pt, sched, ws_s,
                 n_leaf, n_int, E, L):
-    """Training step = jitdb_schedule + jitdb_treelstm_forward_train + jitdb_treelstm_backward, one stream."""
+    """Training step = jitdb_schedule + jitdb_treelstm_forward_train + jitdb_treelstm_backward, one stream.  With --classes
+    the cotangent of h is not given but comes from a loss at every node: layer norm and dropout of h, softmax cross entropy."""
     dt = J.JITDB_BF16 if esz == 2 else J.JITDB_F32
     f32 = dict(dtype=torch.float32, device=dev)
     ws_f = torch.empty(J.jitdb_treelstm_workspace_bytes(N, E, D, H, dt), dtype=torch.uint8, device=dev)
@@ -60,6 +61,29 @@ def train_bench(args, J, torch, cfg, dev, N, D, H, esz, peak_tflops, xt, Wt, Ut,
     grads = (torch.empty((N, D), **f32), torch.empty((4 * H, D), **f32), torch.empty((4 * H, H), **f32),
              torch.empty(4 * H, **f32))
     stream = torch.cuda.current_stream()
+    C, p = args.classes, 0.1
+    if C:
+        gen = torch.Generator().manual_seed(31 + cfg.index)
+        V = (torch.randn((C, H), generator=gen) / H ** 0.5).to(dev, xt.dtype)
+        label = torch.randint(0, C, (N,), generator=gen, dtype=torch.int32).to(dev)
+        gamma, beta, bias = torch.ones(H, **f32), torch.zeros(H, **f32), torch.zeros(C, **f32)
+        state = torch.tensor([cfg.index, 0], dtype=torch.int64, device=dev)      # (a program moves the second on by (N H + 1) / 2 a step)
+        gloss = torch.full((N,), 1.0 / N, **f32)
+        gc = torch.zeros((N, H), **f32)
+        normed = (torch.empty_like(h), torch.empty(N, **f32), torch.empty(N, **f32))
+        losses = (torch.empty(N, **f32), torch.empty(N, **f32))
+        g_loss = (torch.empty_like(h), torch.empty_like(V), torch.empty(C, **f32))
+        g_norm = (gh, torch.empty(H, **f32), torch.empty(H, **f32))
+        ws_h = torch.empty(max(J.jitdb_softmax_xent_workspace_bytes(N, H, C, dt),
+                               J.jitdb_softmax_xent_backward_workspace_bytes(N, H, C, dt, dt),
+                               J.jitdb_layernorm_backward_workspace_bytes(N, H, dt)), dtype=torch.uint8, device=dev)
+
+    def head():
+        y, mean, rstd = J.jitdb_layernorm_forward(h, gamma, beta, p=p, state=state, stream=stream, out=normed)
+        _, lse = J.jitdb_softmax_xent_forward(y, V, label, b=bias, stream=stream, workspace=ws_h, out=losses)
+        dy, _, _ = J.jitdb_softmax_xent_backward(y, V, label, lse, gloss=gloss, b=bias, grad_dtype=h.dtype, stream=stream,
+                                                 workspace=ws_h, out=g_loss)
+        J.jitdb_layernorm_backward(h, gamma, mean, rstd, dy, p=p, state=state, stream=stream, workspace=ws_h, out=g_norm)
 
     def fwd():
         J.jitdb_treelstm_forward_train(xt, Wt, Ut, bt, sched, stream=stream, workspace=ws_f, out=(h, c, gates, fgate))
@@ -71,6 +95,8 @@ def train_bench(args, J, torch, cfg, dev, N, D, H, esz, peak_tflops, xt, Wt, Ut,
     def step():
         J.jitdb_schedule(pt, stream=stream, workspace=ws_s, out=sched)
         fwd()
+        if C:
+            head()
         bwd()
 
     for _ in range(args.warmup):
@@ -92,6 +118,12 @@ def train_bench(args, J, torch, cfg, dev, N, D, H, esz, peak_tflops, xt, Wt, Ut,
         return e0.elapsed_time(e1) / reps
     reps = max(2, min(args.steps, 5))
     ms_f, ms_b = timed(fwd, reps), timed(bwd, reps)
+    head_out = {}
+    if C:
+        mean_loss = losses[0].mean().item()
+        if not np.isfinite(mean_loss):
+            raise SystemExit(f"the loss is {mean_loss}")
+        head_out = {"n_classes": C, "dropout": p, "ms_head": timed(head, reps), "loss": mean_loss}
     # every multiply-add of the forward has two in the backward (data and weight gradient)
     f_min = n_leaf * 2.0 * D * 3 * H + n_int * (2.0 * D * 4 * H + 2.0 * H * 3 * H) + E * 2.0 * H * H
     out = {
@@ -101,9 +133,11 @@ def train_bench(args, J, torch, cfg, dev, N, D, H, esz, peak_tflops, xt, Wt, Ut,
         "data": "synthetic",
         "config": {"workload": f"config {cfg.index}: {cfg.name}", "n_trees": cfg.n_trees, "n_nodes": N, "n_edges": E,
                    "n_levels": L, "D": D, "H": H,
-                   "step": "jitdb_schedule + jitdb_treelstm_forward_train + jitdb_treelstm_backward "
-                           "(cotangents on h and c of every node), one stream"},
-        "ms_forward_train": ms_f, "ms_backward": ms_b,
+                   "step": "jitdb_schedule + jitdb_treelstm_forward_train + "
+                           + ("layer norm, dropout, softmax cross entropy at every node and their gradients + "
+                              "jitdb_treelstm_backward" if C else
+                              "jitdb_treelstm_backward (cotangents on h and c of every node)") + ", one stream"},
+        "ms_forward_train": ms_f, "ms_backward": ms_b, **head_out,
         "roofline": {"kernel": "backward pass as a whole (its products: rows_tile_kernel, tn_kernel)",
                      "bound": "mfma", "achieved": 2.0 * f_min / (ms_b * 1e-3) / 1e12, "peak": peak_tflops,
                      "unit": "TFLOP/s", "frac": 2.0 * f_min / (ms_b * 1e-3) / 1e12 / peak_tflops, "traffic": None,
@@ -289,6 +323,9 @@ def main():
     ap.add_argument("--train", action="store_true",
                     help="time the training step instead (schedule + forward that keeps the gates + backward); "
                          "not the headline metric")
+    ap.add_argument("--classes", type=int, default=0,
+                    help="with --train: a loss over this many classes at every node, behind layer norm and dropout, instead of "
+                         "given cotangents")
     ap.add_argument("--signatures", type=int, default=0,
                     help="time the typed table instead: every tree under one of this many networks "
                          "(jitdb_schedule_typed + jitdb_treelstm_forward_typed); not the headline metric")
