@@ -236,12 +236,13 @@ after_rows_kernel(const PrepArgs a) {
     }
 }
 
-// 64 rows a block; wave w takes every fourth set of statistics, then the four are put together.  The sets are `n_stat` of max_rows
+// 64 rows a block; each of sixteen waves takes every sixteenth set of statistics, then theirs are put together.  The sets are `n_stat` of max_rows
 // rows, or, class_tiles > 0, those that resident_kernel left.
-__global__ void __launch_bounds__(kT)
+constexpr int kJoinWaves = 16;
+__global__ void __launch_bounds__(64 * kJoinWaves)
 join_kernel(const float2 *__restrict__ stat, int n_stat, int class_tiles, int places, int row0, int max_rows, const int32_t *__restrict__ n_rows,
             const int32_t *__restrict__ row_of, const float *__restrict__ label_z, float *__restrict__ loss, float *__restrict__ lse) {
-    __shared__ float2 red[4][64];
+    __shared__ float2 red[kJoinWaves][64];
     const int rows = chunk_rows(n_rows, row0, max_rows);
     if ((int)blockIdx.x * 64 >= rows) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = blockIdx.x * 64 + lane;
@@ -260,11 +261,11 @@ join_kernel(const float2 *__restrict__ stat, int n_stat, int class_tiles, int pl
     };
     if (r < rows)
 #pragma unroll 4
-        for (int k = wave; k < n_stat; k += 4) add(stat[k * stride + r]);
+        for (int k = wave; k < n_stat; k += kJoinWaves) add(stat[k * stride + r]);
     red[wave][lane] = make_float2(top, s);
     __syncthreads();
     if (wave || r >= rows) return;
-    for (int w = 1; w < 4; ++w) add(red[w][lane]);
+    for (int w = 1; w < kJoinWaves; ++w) add(red[w][lane]);
     const float v = top + logf(s);
     const int64_t at = row_of[row0 + r];
     lse[at] = v;
@@ -423,7 +424,7 @@ int run_forward_xent(const T *h, const T *V, const float *b, const RowList &list
         a.res = w.h.at; a.res_slab = w.h.slab; a.str = w.v.at; a.str_slab = w.v.slab; a.side = w.bias;
         a.n_rows = w.n_rows; a.max_rows = (int)s.n_pad; a.class_tiles = s.class_tiles; a.stat = w.stat;
         if ((rc = launch_resident<T, 0>(s.res, res_most(s.n_pad / kResRows, s.class_tiles), a, st)) != JITDB_OK) return rc;
-        join_kernel<<<(unsigned)ceil_div(s.n, 64), kT, 0, st>>>(w.stat, 0, s.class_tiles, res_places(s.parts * s.res, false), 0, a.max_rows, w.n_rows, w.row_of, w.label_z, loss, lse);
+        join_kernel<<<(unsigned)ceil_div(s.n, 64), 64 * kJoinWaves, 0, st>>>(w.stat, 0, s.class_tiles, res_places(s.parts * s.res, false), 0, a.max_rows, w.n_rows, w.row_of, w.label_z, loss, lse);
         JITDB_LAUNCH_CHECK();
         return JITDB_OK;
     }
@@ -437,7 +438,7 @@ int run_forward_xent(const T *h, const T *V, const float *b, const RowList &list
         const int64_t rows = s.n - r0 < s.stat_rows ? s.n - r0 : s.stat_rows;
         wide_logits_kernel<0, sizeof(T) == 4><<<xcd_grid(ceil_div(rows, 256) * a.a_tiles), kTileT<2>, 0, st>>>(a);
         JITDB_LAUNCH_CHECK();
-        join_kernel<<<(unsigned)ceil_div(rows, 64), kT, 0, st>>>(w.stat, 2 * a.a_tiles, 0, 0, a.row0, a.max_rows, w.n_rows, w.row_of, w.label_z, loss, lse);
+        join_kernel<<<(unsigned)ceil_div(rows, 64), 64 * kJoinWaves, 0, st>>>(w.stat, 2 * a.a_tiles, 0, 0, a.row0, a.max_rows, w.n_rows, w.row_of, w.label_z, loss, lse);
         JITDB_LAUNCH_CHECK();
     }
     return JITDB_OK;

@@ -432,27 +432,49 @@ wide_logits_kernel(const LogitArgs a) {
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const float *rec = a.side + (int64_t)(r0 / 32 + t) * 128 + q * 8 + hf * 4;
-                const float4 l4 = *reinterpret_cast<const float4 *>(rec), w4 = *reinterpret_cast<const float4 *>(rec + 32);
-                const int4 n4 = *reinterpret_cast<const int4 *>(rec + 64);
-                const float lse[4] = {l4.x, l4.y, l4.z, l4.w}, w[4] = {w4.x, w4.y, w4.z, w4.w};
-                const int label[4] = {n4.x, n4.y, n4.z, n4.w};
+            for (int qq = 0; qq < 2; ++qq) {             // two quads of rows: the wave's halves exchange them for stores of 16 bytes
+                const float *rec = a.side + (int64_t)(r0 / 32 + t) * 128 + qq * 16 + hf * 4;
+                float lse[2][4], w[2][4];
+                int label[2][4];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    __builtin_memcpy(lse[i], rec + i * 8, 16);
+                    __builtin_memcpy(w[i], rec + i * 8 + 32, 16);
+                    __builtin_memcpy(label[i], rec + i * 8 + 64, 16);
+                }
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    float d[4];
+                    uint32_t words[G][2][2];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float z = acc[t][j][4 * q + e] + own_bias[j];
-                        const float p = CLOSE ? exp_close(z - lse[e]) : __builtin_amdgcn_exp2f(fmaf(z, kLog2e, -lse[e]));
-                        d[e] = (p - (label[e] == c0 + j * 32 ? 1.0f : 0.0f)) * w[e];
-                        colsum[j] += d[e];
+                    for (int i = 0; i < 2; ++i) {
+                        float d[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const float z = acc[t][j][4 * (2 * qq + i) + e] + own_bias[j];
+                            const float p = CLOSE ? exp_close(z - lse[i][e]) : __builtin_amdgcn_exp2f(fmaf(z, kLog2e, -lse[i][e]));
+                            d[e] = (p - (label[i][e] == c0 + j * 32 ? 1.0f : 0.0f)) * w[i][e];
+                            colsum[j] += d[e];
+                        }
+#pragma unroll
+                        for (int k = 0; k < G; ++k)
+#pragma unroll
+                            for (int m = 0; m < 2; ++m) {
+                                const uint32_t y = pack_bf16(d[2 * m], d[2 * m + 1]);
+                                words[k][i][m] = y;
+                                d[2 * m] -= low_bf16(y);
+                                d[2 * m + 1] -= high_bf16(y);
+                            }
                     }
 #pragma unroll
                     for (int k = 0; k < G; ++k) {
-                        const u32x2 y = {pack_bf16(d[0], d[1]), pack_bf16(d[2], d[3])};
-                        __builtin_memcpy(a.g + k * a.g_part + (int64_t)(r0 / 32 + t) * a.g_slab + (int64_t)(c0 + j * 32) * 64 + q * 16 + hf * 8, &y, 8);
-                        d[0] -= low_bf16(y[0]); d[1] -= high_bf16(y[0]); d[2] -= low_bf16(y[1]); d[3] -= high_bf16(y[1]);
+                        u32x4 out;
+#pragma unroll
+                        for (int m = 0; m < 2; ++m) {
+                            const auto s = __builtin_amdgcn_permlane32_swap(words[k][0][m], words[k][1][m], false, false);
+                            out[m] = s[0];
+                            out[2 + m] = s[1];
+                        }
+                        *reinterpret_cast<u32x4 *>(a.g + k * a.g_part + (int64_t)(r0 / 32 + t) * a.g_slab + (int64_t)(c0 + j * 32) * 64 + qq * 32 + hf * 16) = out;
                     }
                 }
             }
