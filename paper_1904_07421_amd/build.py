@@ -348,7 +348,8 @@ def build(verbose: bool = False) -> str:
     for stem, name, expected in (("forward", "12level_kernel", None), ("forward", "14gemm_kb_kernel", None),
                                  ("forward", "17nary_level_kernel", None), ("backward", "16rows_tile_kernel", None),
                                  ("backward", "9tn_kernel", None), ("xent", "19grad_product_kernelILi4E", 4),
-                                 ("xent", "19grad_product_kernelILi2E", 6), ("xent", "18wide_logits_kernel", 6)):
+                                 ("xent", "19grad_product_kernelILi2E", 6), ("xent", "19grad_product_kernelILi5E", 7),
+                                 ("xent", "18wide_logits_kernel", 6)):
         if check_stage_loads(asm_texts[stem], name, expected) == 0:
             raise RuntimeError(f"no K loop with stage loads found in the assembly of {name}: the check is not looking at it")
     if check_walk_loads(asm_texts["xent"], "15resident_kernel") == 0:

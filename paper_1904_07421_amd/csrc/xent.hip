@@ -282,7 +282,7 @@ clear_kernel(O *__restrict__ p, int64_t n) {
 struct Sizes {
     int64_t n, n_pad;          // rows at most, and rounded up to whole tiles
     int H, C, Hk, Hf, Cp;      // widths: of K (states), of the turned states' rows, classes in whole tiles
-    int at;                    // features of a tile of the gradients' products / 64
+    int wm, tile_a, a_tiles, places;      // of the gradients' products: variant, features of a tile, tiles, blocks on the chip
     int parts, g_parts;        // of the operands, of g
     int label_per, label_blocks;
     int res, class_tiles;      // resident_kernel: K in steps of 16 (0: not for this width), tiles of 32 classes
@@ -301,8 +301,18 @@ bool make_sizes(int64_t n, int32_t H, int32_t C, jitdb_dtype dtype, jitdb_dtype 
     s.n_pad = round_up(n > 0 ? n : 1, 256);
     s.res = res_steps(H, dtype);
     s.Hk = s.res ? s.res * 16 : (int)round_up(H, 32);
-    s.at = round_up(H, 128) < round_up(H, 256) ? 2 : 4;
-    s.Hf = (int)round_up(H, 64 * s.at);
+    // The tile height that pads the features least, of equals the highest.  Both gradients' products: bf16 65536 x 150 x 32000 in tiles of
+    // 160 features 1.70 ms, of 256 2.18; fp32 30000 x 300 x 8000 of 160 2.08, of 128 2.34; 30000 x 450 x 8000 of 160 3.21, of 256 3.32.
+    auto take_tile = [&](auto wm) {
+        constexpr int WM = decltype(wm)::value, A = kTileA<WM>;
+        if (s.wm && round_up(H, A) >= (int64_t)s.tile_a * s.a_tiles) return;
+        s.wm = WM; s.tile_a = A; s.a_tiles = (int)ceil_div(H, A); s.places = kTilePlaces<WM>;
+    };
+    s.wm = 0;
+    take_tile(std::integral_constant<int, 4>());
+    take_tile(std::integral_constant<int, 5>());
+    take_tile(std::integral_constant<int, 2>());
+    s.Hf = (int)round_up((int64_t)s.tile_a * s.a_tiles, 64);
     s.Cp = (int)round_up(C, 256);
     s.class_tiles = (int)ceil_div(C, kResTile);
     s.parts = dtype == JITDB_F32 ? 3 : 1;
@@ -324,9 +334,8 @@ int64_t res_most(int64_t blocks, int64_t tiles) {
 }
 // most shares of tiles (grad_plan): of every tile of A, a tile of B more than ranges
 int64_t grad_parts(const Sizes &s, int64_t b_tiles, int64_t nk, int pairs) {
-    const int a_tiles = s.Hf / (64 * s.at);
-    const int64_t most = grad_ranges(s.at == 4 ? kTilePlaces<4> : kTilePlaces<2>, a_tiles), ranges = ceil_div(b_tiles * nk * pairs, kMinStages);
-    return a_tiles * (b_tiles + (ranges < most ? ranges : most));
+    const int64_t most = grad_ranges(s.places, s.a_tiles), ranges = ceil_div(b_tiles * nk * pairs, kMinStages);
+    return s.a_tiles * (b_tiles + (ranges < most ? ranges : most));
 }
 int pair_count(int a, int b) { return a == 3 && b == 3 ? 6 : a * b; }        // (one part and three: three products)
 struct Space {
@@ -361,7 +370,7 @@ Space carve(const Sizes &s, bool backward, void *base) {
         w.ht = take_operand(c, s.parts, s.n_pad / 32, s.Hf);
         w.g = take_operand(c, s.g_parts, s.grad_rows / 32, s.Cp);
         w.db_part = c.take<float>(s.res ? (size_t)res_most(s.Cp / kResRows, s.grad_rows / kResTile) * kResRows : (size_t)(s.grad_rows / 64) * s.Cp);
-        const int pairs = pair_count(s.parts, s.g_parts), tile = 64 * s.at * kTileB;
+        const int pairs = pair_count(s.parts, s.g_parts), tile = s.tile_a * kTileB;
         w.part_h = c.take<float>((size_t)(grad_parts(s, s.grad_rows / kTileB, ceil_div(s.C, 32), pairs) * tile));
         w.part_v = c.take<float>((size_t)(grad_parts(s, ceil_div(s.C, kTileB), s.grad_rows / 32, pairs) * tile));
         if (s.grad_rows < s.n) w.acc_v = c.take<float>((size_t)s.C * s.H);
@@ -429,7 +438,7 @@ int run_forward_xent(const T *h, const T *V, const float *b, const RowList &list
         return JITDB_OK;
     }
     LogitArgs a = {};
-    a.p.A = w.v; a.p.B = w.h; a.p.pairs = make_pairs(w.v, s.parts, w.h, s.parts);
+    a.p.A = w.v; a.p.B = w.h; a.p.pairs = make_pairs(s.parts, s.parts);
     a.nk = s.Hk / 32; a.a_tiles = s.Cp / 128; a.n_rows = w.n_rows; a.bias = w.bias; a.stat = w.stat;
     a.max_rows = s.stat_rows;
     for (int64_t r0 = 0; r0 < s.n; r0 += s.stat_rows) {
@@ -447,7 +456,7 @@ int run_forward_xent(const T *h, const T *V, const float *b, const RowList &list
 // dh, dV and db of one chunk of rows
 template <int WM, typename O>
 int run_grad_products(int64_t row_tiles, const GradArgs &gh, const GradArgs &gv, BiasArgs bias, hipStream_t st) {
-    const int64_t ranges = grad_ranges(kTilePlaces<WM>, gh.a_tiles), pieces = gh.a_tiles * (row_tiles + ceil_div(gv.C, kTileB)) * 8 + ceil_div(gv.C, 64);
+    const int64_t ranges = grad_ranges(kTilePlaces<WM>, gh.a_tiles), pieces = gh.a_tiles * (row_tiles + ceil_div(gv.C, kTileB)) * (kTM<WM> * kTN<WM>) + ceil_div(gv.C, 64);
     const unsigned half = xcd_grid(ranges * gh.a_tiles);
     grad_product_kernel<WM><<<2 * half, kTileT<WM>, 0, st>>>(gh, gv, (int)half);
     JITDB_LAUNCH_CHECK();
@@ -466,15 +475,15 @@ int run_backward_xent(const T *h, const T *V, const float *b, const RowList &lis
     ra.res = w.v.at; ra.res_slab = w.v.slab; ra.str_slab = w.h.slab; ra.n_rows = w.n_rows; ra.max_rows = s.grad_rows;
     ra.class_blocks = s.Cp / kResRows; ra.bias = w.bias; ra.g = w.g.at; ra.g_slab = w.g.slab; ra.g_part = w.g.part; ra.db_part = w.db_part;
     LogitArgs a = {};
-    a.p.A = w.h; a.p.B = w.v; a.p.pairs = make_pairs(w.h, s.parts, w.v, s.parts);
+    a.p.A = w.h; a.p.B = w.v; a.p.pairs = make_pairs(s.parts, s.parts);
     a.nk = s.Hk / 32; a.b_tiles = s.Cp / 256; a.n_rows = w.n_rows; a.max_rows = s.grad_rows; a.bias = w.bias;
     a.g = w.g.at; a.g_slab = w.g.slab; a.g_part = w.g.part; a.db_part = w.db_part;
     GradArgs gh = {}, gv = {};
-    gh.p.A = w.v; gh.p.B = w.g; gh.p.pairs = make_pairs(w.v, s.parts, w.g, s.g_parts); gh.p.a_slabs = s.Hk / 32; gh.p.b_slabs = s.grad_rows / 32;
+    gh.p.A = w.v; gh.p.B = w.g; gh.p.pairs = make_pairs(s.parts, s.g_parts); gh.p.a_slabs = s.Hk / 32; gh.p.b_slabs = s.grad_rows / 32;
     gh.part = w.part_h; gh.out = dh; gh.row_of = w.row_of;
-    gv.p.A = w.ht; gv.p.B = w.g; gv.p.pairs = make_pairs(w.ht, s.parts, w.g, s.g_parts);
+    gv.p.A = w.ht; gv.p.B = w.g; gv.p.pairs = make_pairs(s.parts, s.g_parts);
     gv.part = w.part_v; gv.out = dV; gv.acc = w.acc_v;
-    for (GradArgs *g : {&gh, &gv}) { g->a_tiles = s.Hf / (64 * s.at); g->n_rows = w.n_rows; g->max_rows = s.grad_rows; g->H = s.H; g->C = s.C; }
+    for (GradArgs *g : {&gh, &gv}) { g->a_tiles = s.a_tiles; g->n_rows = w.n_rows; g->max_rows = s.grad_rows; g->H = s.H; g->C = s.C; }
     for (int64_t r0 = 0; r0 < s.n; r0 += s.grad_rows) {
         const int64_t rows = s.n - r0 < s.grad_rows ? s.n - r0 : s.grad_rows, row_tiles = ceil_div(rows, 256);
         ra.row0 = a.row0 = gh.row0 = gv.row0 = (int)r0;
@@ -490,7 +499,8 @@ int run_backward_xent(const T *h, const T *V, const float *b, const RowList &lis
         }
         gv.p.A.at = w.ht.at + r0 / 32 * w.ht.slab;
         const BiasArgs bias = {w.db_part, db, s.Cp, s.res ? res_places(s.parts * s.res, true) : 0};
-        rc = s.at == 4 ? run_grad_products<4, O>(row_tiles, gh, gv, bias, st) : run_grad_products<2, O>(row_tiles, gh, gv, bias, st);
+        rc = s.wm == 4 ? run_grad_products<4, O>(row_tiles, gh, gv, bias, st) : s.wm == 5 ? run_grad_products<5, O>(row_tiles, gh, gv, bias, st)
+                                                                                          : run_grad_products<2, O>(row_tiles, gh, gv, bias, st);
         if (rc != JITDB_OK) return rc;
     }
     return JITDB_OK;

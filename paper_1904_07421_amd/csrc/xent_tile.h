@@ -1,10 +1,10 @@
 // C = A^T B or A B^T in tiles, both operands streaming through LDS: the gradients' products, and logits of wide states.
 //
-// 2 WM waves multiply a tile of 64 WM rows of A (128 or 256) and 256 rows of B; each 2 x 4 MFMA tiles of 32 x 32.  In a 32 x 32 tile
-// lane l holds row l % 32 of B and rows 8 q + 4 (l / 32) + e of A (q, e < 4).  K runs over stages of 64 bytes a row (32 bf16) that travel
-// straight into LDS, one barrier a stage.  K_ROWS: the reduction runs over the operands' rows instead (32 a stage; a tile takes slabs of 32
-// columns each), transposed on the way out of LDS.  Two waves share a SIMD: eight of a block with WM = 4, of two blocks with WM = 2 (for
-// operands of at most 128 rows).  (Four waves of twice the size, alone on their SIMDs, read less LDS and were no faster.)
+// A block multiplies a tile of kTileA rows of A (128, 160 or 256) and 256 rows of B; each wave TM x TN MFMA tiles of 32 x 32.  In such a
+// tile lane l holds row l % 32 of B and rows 8 q + 4 (l / 32) + e of A (q, e < 4).  K runs over stages of 64 bytes a row (32 bf16) that
+// travel straight into LDS, one barrier a stage.  K_ROWS: the reduction runs over the operands' rows instead (32 a stage; a tile takes
+// slabs of 32 columns each), transposed on the way out of LDS.  Two waves share a SIMD: eight of a block of 256 rows, else of two blocks of
+// four.  (Four waves of twice the size, alone on their SIMDs, read less LDS and were no faster.)
 // A direct load writes the 64 lanes' pieces to 1024 consecutive LDS bytes, 16 rows of 64: piece p of row r is kept in slot
 // p ^ ((r >> 2) & 3), so that a fragment read of 16 rows touches 16 distinct 16-byte columns.
 #pragma once
@@ -16,12 +16,15 @@ namespace {
 
 constexpr int kTileB = 256;                           // rows of B in a tile
 constexpr int kT = 256;                               // threads of the small kernels
-constexpr int kMaxPairs = 6;
-template <int WM> constexpr int kTileA = 64 * WM;     // rows of A
-template <int WM> constexpr int kTileT = 128 * WM;    // threads
+template <int WM> constexpr int kTileA = WM * 64;     // rows of A; WM: 64-row waves along A (5: four waves along B with all 160)
+template <> constexpr int kTileA<5> = 160;
+template <int WM> constexpr int kTM = WM == 5 ? 5 : 2;
+template <int WM> constexpr int kTN = WM == 5 ? 2 : 4;
+template <int WM> constexpr int kTileT = WM == 4 ? 512 : 256;           // threads
 template <int WM> constexpr int kTileBufs = WM == 4 ? 4 : 3;
 template <int WM> constexpr int kTileBuf = (kTileA<WM> + kTileB) * 64;
 template <int WM> constexpr int kTilePlaces = WM == 4 ? 256 : 512;      // blocks the chip holds at once
+template <int WM> constexpr int kTileWaves = WM == 4 ? 1 : 2;           // blocks on a CU
 
 // Operands are K-blocked as in operand_offset, in one to three bf16 parts: part p, slab s (32 elements of K), row r
 // at + p * part + s * slab + r * 64.
@@ -29,17 +32,16 @@ struct Operand {
     char *at;
     int64_t slab, part;
 };
-// The part products of one product, smallest first: where the parts lie behind each operand's first.  (Whole words: the
-// compiler reads them with scalar loads, which the K loop's hand-counted waits for vector memory do not see.)
+// The part products of one product, smallest first: four bits each, which part of A and of B.
 struct Pairs {
-    int64_t a[kMaxPairs], b[kMaxPairs];
+    uint32_t code;
     int n;
 };
-inline Pairs make_pairs(const Operand &a, int parts_a, const Operand &b, int parts_b) {
+inline Pairs make_pairs(int parts_a, int parts_b) {
     Pairs p = {};
     for (int w = 2; w >= 0; --w)
         for (int i = 0; i <= w; ++i)
-            if (i < parts_a && w - i < parts_b) { p.a[p.n] = i * a.part; p.b[p.n] = (w - i) * b.part; ++p.n; }
+            if (i < parts_a && w - i < parts_b) p.code |= (uint32_t)(i | (w - i) << 2) << (4 * p.n++);
     return p;
 }
 struct Product {
@@ -48,21 +50,27 @@ struct Product {
     int a_slabs, b_slabs;           // K_ROWS: slabs there are; what lies behind the last is never read
 };
 
-// acc += stages s0 .. s0 + n_stages (n_stages >= 1) of the `nk` stages of each part product, one product behind the other; a0, b0: the
-// tile's first row of each operand (K_ROWS: first slab)
+// acc += stages s0 .. s0 + n_stages (n_stages >= 1); a0, b0: the tile's first row of each operand (K_ROWS: first slab).  The part products
+// of 32 elements of K follow one another, so that each part comes from memory once and from L2 after that (both gradients' products, fp32
+// 8192 x 160 x 10000: 338 us; with one part product behind the other, which read g twice as often, 426)
 template <bool K_ROWS, int WM>
-__device__ __forceinline__ void multiply_tile(const Product &p, int64_t a0, int64_t b0, int nk, int s0, int n_stages, char *lds, floatx16 (&acc)[2][4]) {
-    constexpr int A_UNITS = 4 * WM, LOADS = (A_UNITS + 16) / (2 * WM), BUFS = kTileBufs<WM>, BUF = kTileBuf<WM>, B_AT = A_UNITS * 1024;
+__device__ __forceinline__ void multiply_tile(const Product &p, int64_t a0, int64_t b0, int s0, int n_stages, char *lds, floatx16 (&acc)[kTM<WM>][kTN<WM>]) {
+    constexpr int TM = kTM<WM>, TN = kTN<WM>, WAVES = kTileT<WM> / 64, WAVES_N = kTileB / (32 * TN);
+    constexpr int A_UNITS = kTileA<WM> / 16, UNITS = A_UNITS + kTileB / 16, LOADS = (UNITS + WAVES - 1) / WAVES, BUFS = kTileBufs<WM>, BUF = kTileBuf<WM>, B_AT = A_UNITS * 1024;
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int wm = wave >> 1, wn = wave & 1, hf = lane >> 5, l32 = lane & 31, lrow = lane >> 2;
+    const int wm = wave / WAVES_N, wn = wave % WAVES_N, hf = lane >> 5, l32 = lane & 31, lrow = lane >> 2;
     // movers: 1 KB units of 16 rows of a slab, those of A in front of those of B, LOADS a wave (scalar addresses and one offset for
     // every lane: no vector instruction is spent on them)
     const uint32_t lane_off = lrow * 64 + (K_ROWS ? lane & 3 : (lane & 3) ^ ((lane >> 4) & 3)) * 16;
     const char *from[LOADS];
+    auto unit = [&](int i) __attribute__((always_inline)) {         // (the last wave's last may come twice: every wave issues as many)
+        const int u = wave * LOADS + i;
+        return UNITS % WAVES == 0 || u < UNITS ? u : UNITS - 1;
+    };
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
-        const int u = wave * LOADS + i, v = u < A_UNITS ? u : u - A_UNITS;
+        const int u = unit(i), v = u < A_UNITS ? u : u - A_UNITS;
         const Operand &o = u < A_UNITS ? p.A : p.B;
         const int64_t first = u < A_UNITS ? a0 : b0;
         if constexpr (K_ROWS) {
@@ -74,40 +82,44 @@ __device__ __forceinline__ void multiply_tile(const Product &p, int64_t a0, int6
         }
     }
     const int64_t a_stage = K_ROWS ? 32 * 64 : p.A.slab, b_stage = K_ROWS ? 32 * 64 : p.B.slab;
-    int q = s0 / nk, k = s0 - q * nk, issued = 0;
-    int64_t a_off = p.pairs.a[q] + k * a_stage, b_off = p.pairs.b[q] + k * b_stage;
+    int k = s0 / p.pairs.n, q = s0 - k * p.pairs.n, issued = 0;
+    int64_t a_at = k * a_stage, b_at = k * b_stage, a_off, b_off;
+    auto take_part = [&]() __attribute__((always_inline)) {
+        const uint32_t i = p.pairs.code >> (4 * q) & 3, j = p.pairs.code >> (4 * q + 2) & 3;
+        a_off = a_at + (i == 0 ? 0 : i == 1 ? p.A.part : 2 * p.A.part);
+        b_off = b_at + (j == 0 ? 0 : j == 1 ? p.B.part : 2 * p.B.part);
+    };
+    take_part();
     auto issue_one = [&](int buf, int i) __attribute__((always_inline)) {
-        const int u = wave * LOADS + i;
+        const int u = unit(i);
         const char *at = from[i] + (u < A_UNITS ? a_off : b_off);
         __builtin_amdgcn_global_load_lds(JITDB_GLOBAL_PTR(at + lane_off), JITDB_LDS_PTR(lds + buf * BUF + u * 1024), 16, 0, 0);
     };
     auto advance = [&]() __attribute__((always_inline)) {        // behind the last stage the last one is asked for again: the waits count on it
         if (++issued >= n_stages) return;
-        a_off += a_stage;
-        b_off += b_stage;
-        if (++k == nk) {
-            k = 0;
-            ++q;
-            a_off = p.pairs.a[q];
-            b_off = p.pairs.b[q];
+        if (++q == p.pairs.n) {
+            q = 0;
+            a_at += a_stage;
+            b_at += b_stage;
         }
+        take_part();
     };
     int a_rd[2], b_rd[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         if constexpr (K_ROWS) {
             const int at = h * 1024 + (hf * 4 + ((lane & 15) >> 2)) * 64 + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
-            a_rd[h] = wm * 4096 + at;
-            b_rd[h] = B_AT + wn * 8192 + at;
+            a_rd[h] = wm * TM * 2048 + at;
+            b_rd[h] = B_AT + wn * TN * 2048 + at;
         } else {
             const int slot16 = ((2 * h + hf) ^ ((l32 >> 2) & 3)) * 16;
-            a_rd[h] = (wm * 64 + l32) * 64 + slot16;
-            b_rd[h] = B_AT + (wn * 128 + l32) * 64 + slot16;
+            a_rd[h] = wm * TM * 2048 + l32 * 64 + slot16;
+            b_rd[h] = B_AT + wn * TN * 2048 + l32 * 64 + slot16;
         }
     }
     const uint32_t lds_base = (uint32_t)(uintptr_t)JITDB_LDS_PTR(lds);
     struct Frags {
-        u32x4 a[2], b[4];
+        u32x4 a[TM], b[TN];
     };
     // tiles of 32 rows lie 2048 bytes apart in either layout
     auto read_one = [&](auto tile, uint32_t at, u32x4 &f) __attribute__((always_inline)) {
@@ -123,23 +135,26 @@ __device__ __forceinline__ void multiply_tile(const Product &p, int64_t a0, int6
     };
     auto read_group = [&](int buf, int h, Frags &f) __attribute__((always_inline)) {
         const uint32_t aa = lds_base + buf * BUF + a_rd[h], bb = lds_base + buf * BUF + b_rd[h];
-        static_for<4>([&](auto i) __attribute__((always_inline)) {
-            if constexpr (decltype(i)::value < 2) read_one(i, aa, f.a[decltype(i)::value]);
-            read_one(i, bb, f.b[decltype(i)::value]);
+        static_for<(TM > TN ? TM : TN)>([&](auto i) __attribute__((always_inline)) {
+            if constexpr (decltype(i)::value < TM) read_one(i, aa, f.a[decltype(i)::value]);
+            if constexpr (decltype(i)::value < TN) read_one(i, bb, f.b[decltype(i)::value]);
         });
     };
     auto reads_done = [&](Frags &f) __attribute__((always_inline)) {
-        asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(f.a[0]), "+v"(f.a[1]), "+v"(f.b[0]), "+v"(f.b[1]), "+v"(f.b[2]), "+v"(f.b[3]));
+        if constexpr (TM == 2)
+            asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(f.a[0]), "+v"(f.a[1]), "+v"(f.b[0]), "+v"(f.b[1]), "+v"(f.b[2]), "+v"(f.b[3]));
+        else
+            asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(f.a[0]), "+v"(f.a[1]), "+v"(f.a[2]), "+v"(f.a[3]), "+v"(f.a[4]), "+v"(f.b[0]), "+v"(f.b[1]));
     };
     auto multiply = [&](const Frags &f) __attribute__((always_inline)) {
 #pragma unroll
-        for (int m = 0; m < 8; ++m) mfma_step<bf16_t>(f.a[m / 4], f.b[m % 4], acc[m / 4][m % 4]);
+        for (int m = 0; m < TM * TN; ++m) mfma_step<bf16_t>(f.a[m / TN], f.b[m % TN], acc[m / TN][m % TN]);
     };
     // the next requests are dealt out between the MFMAs: a burst of them would hold the wave back until the memory pipeline took them
     auto multiply_and_issue = [&](const Frags &f, int buf) __attribute__((always_inline)) {
 #pragma unroll
-        for (int m = 0; m < 8; ++m) {
-            mfma_step<bf16_t>(f.a[m / 4], f.b[m % 4], acc[m / 4][m % 4]);
+        for (int m = 0; m < TM * TN; ++m) {
+            mfma_step<bf16_t>(f.a[m / TN], f.b[m % TN], acc[m / TN][m % TN]);
             __builtin_amdgcn_sched_barrier(0);
             if (m < LOADS) issue_one(buf, m);
             __builtin_amdgcn_sched_barrier(0);
@@ -182,11 +197,12 @@ __device__ __forceinline__ void multiply_tile(const Product &p, int64_t a0, int6
     wait_barrier(none_left);             // nothing is on its way into the buffers, and every wave is done with them
 }
 
-__device__ __forceinline__ void clear_tile(floatx16 (&acc)[2][4]) {
+template <int TM, int TN>
+__device__ __forceinline__ void clear_tile(floatx16 (&acc)[TM][TN]) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < TM; ++i)
 #pragma unroll
-        for (int g = 0; g < 4; ++g)
+        for (int g = 0; g < TN; ++g)
 #pragma unroll
             for (int v = 0; v < 16; ++v) acc[i][g][v] = 0.0f;
 }
@@ -248,44 +264,45 @@ __device__ __forceinline__ void grad_product(const GradArgs &a, char *lds, int b
     const uint32_t end = s + g.per < g.total ? s + g.per : g.total;
     while (s < end) {
         const uint32_t bt = s / g.stages, s0 = s - bt * g.stages, n = end - s < g.stages - s0 ? end - s : g.stages - s0;
-        floatx16 acc[2][4];
+        floatx16 acc[kTM<WM>][kTN<WM>];
         clear_tile(acc);
-        if constexpr (WEIGHTS) multiply_tile<false, WM>(a.p, (int64_t)at * kTileA<WM>, (int64_t)bt * kTileB, g.nk, s0, n, lds, acc);
-        else multiply_tile<true, WM>(a.p, (int64_t)at * (kTileA<WM> / 32), (int64_t)bt * (kTileB / 32), g.nk, s0, n, lds, acc);
+        if constexpr (WEIGHTS) multiply_tile<false, WM>(a.p, (int64_t)at * kTileA<WM>, (int64_t)bt * kTileB, s0, n, lds, acc);
+        else multiply_tile<true, WM>(a.p, (int64_t)at * (kTileA<WM> / 32), (int64_t)bt * (kTileB / 32), s0, n, lds, acc);
         float4 *out = reinterpret_cast<float4 *>(a.part + ((int64_t)(bt + range) * a.a_tiles + at) * (kTileA<WM> * kTileB)) + threadIdx.x;
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < kTM<WM>; ++i)
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
+            for (int j = 0; j < kTN<WM>; ++j)
 #pragma unroll
                 for (int v = 0; v < 4; ++v)
-                    out[((i * 4 + j) * 4 + v) * kTileT<WM>] = make_float4(acc[i][j][4 * v], acc[i][j][4 * v + 1], acc[i][j][4 * v + 2], acc[i][j][4 * v + 3]);
+                    out[((i * kTN<WM> + j) * 4 + v) * kTileT<WM>] = make_float4(acc[i][j][4 * v], acc[i][j][4 * v + 1], acc[i][j][4 * v + 2], acc[i][j][4 * v + 3]);
         s += n;
     }
 }
 // The first `half` blocks (a multiple of 8) compute dh, as many more dV: where one leaves places on the chip, the other takes them.
 template <int WM>
-__global__ void __launch_bounds__(kTileT<WM>, 4 / WM)
+__global__ void __launch_bounds__(kTileT<WM>, kTileWaves<WM>)
 grad_product_kernel(const GradArgs h, const GradArgs v, int half) {
     __shared__ __attribute__((aligned(1024))) char lds[kTileBufs<WM> * kTileBuf<WM>];
     if ((int)blockIdx.x < half) grad_product<false, WM>(h, lds, blockIdx.x);
     else grad_product<true, WM>(v, lds, blockIdx.x - half);
 }
-// A tile's shares are put together in 8 pieces; a lane writes 32 features of its row or class, the wave's halves taking every other
+// A tile's shares are put together in a piece for each of a wave's MFMA tiles; a lane writes 32 features of its row or class, the wave's halves taking every other
 // four, so that what a block writes of a row is at least half a line (512 x 32000 bf16: 81 us; pieces of four features, whose lines several XCDs share: 127 us
 // in this loop).
 template <bool WEIGHTS, int WM, typename O>
 __device__ __forceinline__ void grad_finish(const GradArgs &a, const GradPlan &g, int64_t piece) {
-    const int i = (int)(piece >> 2) & 1, j = (int)piece & 3, t = threadIdx.x;
-    const uint32_t tile = (uint32_t)(piece >> 3), bt = tile / (uint32_t)a.a_tiles, at = tile - bt * a.a_tiles;
+    constexpr int TM = kTM<WM>, TN = kTN<WM>, WAVES_N = kTileB / (32 * TN);
+    const int t = threadIdx.x;
+    const uint32_t tile = (uint32_t)piece / (TM * TN), ij = (uint32_t)piece % (TM * TN), i = ij / TN, j = ij % TN, bt = tile / (uint32_t)a.a_tiles, at = tile - bt * a.a_tiles;
     const int lane = t & 63, wave = t >> 6;
-    const int m0 = at * kTileA<WM> + (wave >> 1) * 64 + i * 32 + (lane >> 5) * 4;                // first feature, and 8, 16, 24 on
-    const int n = bt * kTileB + (wave & 1) * 128 + j * 32 + (lane & 31);                          // row or class
+    const int m0 = at * kTileA<WM> + wave / WAVES_N * (TM * 32) + i * 32 + (lane >> 5) * 4;                // first feature, and 8, 16, 24 on
+    const int n = bt * kTileB + wave % WAVES_N * (TN * 32) + j * 32 + (lane & 31);                          // row or class
     if (m0 >= a.H || n >= (WEIGHTS ? a.C : chunk_rows(a.n_rows, a.row0, a.max_rows))) return;
     float s[4][4] = {};
     if (g.stages > 0) {
         const uint32_t first = bt * g.stages / g.per, last = ((bt + 1) * g.stages - 1) / g.per;
-        const float4 *in = reinterpret_cast<const float4 *>(a.part + ((int64_t)(bt + first) * a.a_tiles + at) * (kTileA<WM> * kTileB)) + (i * 4 + j) * 4 * kTileT<WM> + t;
+        const float4 *in = reinterpret_cast<const float4 *>(a.part + ((int64_t)(bt + first) * a.a_tiles + at) * (kTileA<WM> * kTileB)) + ij * 4 * kTileT<WM> + t;
 #pragma unroll 2
         for (uint32_t k = first; k <= last; ++k) {
 #pragma unroll
@@ -350,15 +367,16 @@ __device__ __forceinline__ void bias_finish(const BiasArgs &b, const GradArgs &a
 template <int WM, typename O>
 __global__ void __launch_bounds__(kTileT<WM>)
 grad_finish_kernel(const GradArgs h, const GradArgs v, const BiasArgs bias) {
-    __shared__ float sums[2 * WM][64];
+    constexpr int WAVES = kTileT<WM> / 64, PIECES = kTM<WM> * kTN<WM>;
+    __shared__ float sums[WAVES][64];
     const int rows = chunk_rows(h.n_rows, h.row0, h.max_rows);
     if (rows == 0 && h.row0 > 0) return;                         // the chunks before have had all rows
     const GradPlan gh = grad_plan<false, WM>(h), gv = grad_plan<true, WM>(v);
-    const int64_t n_h = (int64_t)gh.b_tiles * h.a_tiles * 8, n_v = (int64_t)gv.b_tiles * v.a_tiles * 8, n = n_h + n_v + (v.C + 63) / 64;
+    const int64_t n_h = (int64_t)gh.b_tiles * h.a_tiles * PIECES, n_v = (int64_t)gv.b_tiles * v.a_tiles * PIECES, n = n_h + n_v + (v.C + 63) / 64;
     for (int64_t i = blockIdx.x; i < n; i += gridDim.x) {
         if (i < n_h) grad_finish<false, WM, O>(h, gh, i);
         else if (i < n_h + n_v) grad_finish<true, WM, O>(v, gv, i - n_h);
-        else bias_finish<2 * WM>(bias, v, rows, (int)(i - n_h - n_v) * 64, sums);
+        else bias_finish<WAVES>(bias, v, rows, (int)(i - n_h - n_v) * 64, sums);
     }
 }
 
@@ -390,7 +408,7 @@ wide_logits_kernel(const LogitArgs a) {
     floatx16 acc[2][4];
     clear_tile(acc);
     const int n_stages = a.nk * a.p.pairs.n;
-    multiply_tile<false, 2>(a.p, (int64_t)(G == 0 ? ct : rt) * 128, (int64_t)(G == 0 ? rt : ct) * 256, a.nk, 0, n_stages, lds, acc);
+    multiply_tile<false, 2>(a.p, (int64_t)(G == 0 ? ct : rt) * 128, (int64_t)(G == 0 ? rt : ct) * 256, 0, n_stages, lds, acc);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave >> 1, wn = wave & 1, hf = lane >> 5, l32 = lane & 31;
     if constexpr (G == 0) {
         const int c0 = ct * 128 + wm * 64;
