@@ -259,7 +259,7 @@ resident_kernel(const ResArgs a) {
 #pragma unroll
                 for (int v = 0; v < 16; ++v) again += expf(z[j][v] - from);
                 sum[j] = out ? again : sum[j];
-                ref[j] = out ? from : ref[j];
+                ref[j] = out ? m : ref[j];                               // (stays -inf until a class is not masked)
                 ref_l[j] = ref[j] * kLog2e;
             }
 #pragma unroll
@@ -306,7 +306,8 @@ resident_kernel(const ResArgs a) {
             }
         });
     };
-    // Labels among the wave's classes, seldom: the derivative of a label's own logit goes out once more, after the others.
+    // Labels among the wave's classes, seldom: the derivative of a label's own logit goes out once more, after the others (a wave's
+    // stores to one place take effect in order).
     auto derivatives_end = [&](floatx16 (&z)[2], int tile) __attribute__((always_inline)) {
         const int first = rb * kResRows + wave * 64;
         uint64_t hits = __ballot(label >= first && label < first + 64) & 0xFFFFFFFFull;      // (both halves hold all 32)
@@ -458,7 +459,7 @@ resident_kernel(const ResArgs a) {
     if constexpr (G == 0) {
 #pragma unroll
         for (int j = 0; j < 2; ++j) {        // the two lanes of a row
-            const float ref2 = __shfl_xor(ref[j], 32), sum2 = __shfl_xor(kept[j], 32), m = fmaxf(ref[j], ref2);
+            const float ref2 = __shfl_xor(ref[j], 32), sum2 = __shfl_xor(kept[j], 32), top = fmaxf(ref[j], ref2), m = top == -INFINITY ? 0.0f : top;
             const float s = kept[j] * expf(ref[j] - m) + sum2 * expf(ref2 - m);
             if (hf == 0) a.stat[((int64_t)range * blocks + rb) * kResRows + wave * 64 + j * 32 + l32] = make_float2(m, s);
         }

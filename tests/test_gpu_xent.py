@@ -361,3 +361,37 @@ def test_a_whole_training_step(dtype):
     for name, got, ref in zip(("dx", "dW", "dU", "db"), (dx, dW, dU, d_bias), want):
         rel = np.linalg.norm(_host(got) - ref) / np.linalg.norm(ref)
         assert rel <= tol, (name, rel)
+
+
+@pytest.mark.parametrize("dtype,grad", KINDS)
+@pytest.mark.parametrize("H", [129, 160, 161, 300, 320, 321, 450])
+def test_widths_around_the_tiles_of_160_features(H, dtype, grad):
+    _check(70, H, 300, dtype, grad)
+
+
+@pytest.mark.parametrize("dtype,grad", KINDS)
+@pytest.mark.parametrize("H,C,first", [(150, 40, 20), (64, 500, 300), (150, 300, 40), (600, 500, 300)])
+def test_first_classes_masked_and_the_others_far_below_zero(H, C, first, dtype, grad):
+    """exp of the logits themselves is 0 in fp32: only a reference among the classes that count finds their sum."""
+    import torch
+    import paper_1904_07421_amd as J
+    print(f"xent H={H} C={C} {first} masked {dtype}/{grad}", flush=True)
+    n = 67
+    rng = np.random.default_rng([H, C, first])
+    h_t, h = _to(rng.uniform(-1, 1, (n, H)), dtype)
+    V_t, V = _to(rng.standard_normal((C, H)) / np.sqrt(H), dtype)
+    label = rng.integers(first, C, n)
+    b = np.full(C, -200.0, np.float32)
+    b[:first] = -np.inf
+    h, V = h.astype(np.float64), V.astype(np.float64)
+    loss_t, lse_t = J.jitdb_softmax_xent_forward(h_t, V_t, _i32(label), b=_f32(b))
+    got = J.jitdb_softmax_xent_backward(h_t, V_t, _i32(label), lse_t, b=_f32(b), grad_dtype=torch.float32 if grad == "f32" else torch.bfloat16)
+    gloss = np.ones(n)
+    loss, lse = O.softmax_xent(h, V, b.astype(np.float64), label)
+    dh, dV, db, g, p = O.softmax_xent_backward(h, V, b.astype(np.float64), label, gloss)
+    loss_err, lse_err, dh_err, dV_err, db_err, out = _tolerances(h, V, b, label, gloss, grad, dtype, loss, lse, g, p)
+    assert np.all(np.abs(_host(lse_t) - lse) <= lse_err)
+    assert np.all(np.abs(_host(loss_t) - loss) <= loss_err)
+    for name, t, want, err in zip(("dh", "dV", "db"), got, (dh, dV, db), (dh_err, dV_err, db_err)):
+        o = U32 if name == "db" else out
+        assert np.all(np.abs(_host(t) - want) <= err * (1 + o) + o * np.abs(want) + 1e-36), name
