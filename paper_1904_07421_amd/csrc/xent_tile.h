@@ -280,6 +280,7 @@ __device__ __forceinline__ void grad_product(const GradArgs &a, char *lds, int b
     }
 }
 // The first `half` blocks (a multiple of 8) compute dh, as many more dV: where one leaves places on the chip, the other takes them.
+// 32768 x 512 x 50021 bf16: 3.24 ms, 1.04 PFLOP/s, of 1.54 that a large library product reaches; the clock falls to 1.6 - 1.85 GHz under it.
 template <int WM>
 __global__ void __launch_bounds__(kTileT<WM>, kTileWaves<WM>)
 grad_product_kernel(const GradArgs h, const GradArgs v, int half) {
@@ -287,9 +288,9 @@ grad_product_kernel(const GradArgs h, const GradArgs v, int half) {
     if ((int)blockIdx.x < half) grad_product<false, WM>(h, lds, blockIdx.x);
     else grad_product<true, WM>(v, lds, blockIdx.x - half);
 }
-// A tile's shares are put together in a piece for each of a wave's MFMA tiles; a lane writes 32 features of its row or class, the wave's halves taking every other
-// four, so that what a block writes of a row is at least half a line (512 x 32000 bf16: 81 us; pieces of four features, whose lines several XCDs share: 127 us
-// in this loop).
+// A tile's shares are put together in a piece for each of a wave's MFMA tiles; a lane writes 32 features of its row or class, the wave's
+// halves taking every other four, so that a block writes at least half a line of a row (32768 x 512 x 50021 bf16: 81 us; in pieces of
+// four features, whose lines several XCDs share, 127).
 template <bool WEIGHTS, int WM, typename O>
 __device__ __forceinline__ void grad_finish(const GradArgs &a, const GradPlan &g, int64_t piece) {
     constexpr int TM = kTM<WM>, TN = kTN<WM>, WAVES_N = kTileB / (32 * TN);
