@@ -7,7 +7,7 @@
 // gradients leave at once.  The weights' gradients sum over rows: the 64 rows of a block put their g into LDS, and each wave adds them
 // to its own quarter of the features, reading the states a second time out of L2, now with a feature in each lane.  Blocks keep their
 // sums in registers to the end; few_reduce_kernel adds the blocks in order.
-// 1.18 M rows of 512, 5 classes, bf16: forward 240 us (5.0 TB/s), backward with fp32 dh 940 (3.9 TB/s).
+// 1.18 M rows of 512, 5 classes, bf16: forward 240 us (5.0 TB/s), backward with fp32 dh 785 (4.6 TB/s; 945 with half lines stored).
 #pragma once
 
 #include "level_common.h"
@@ -214,14 +214,18 @@ few_backward_kernel(const FewArgs a) {
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) *reinterpret_cast<floatx4 *>(&gs[turn][wave * 16 + i16][ct * 16 + q * 4]) = g[ct];
         if (q == 0) has_of[turn][wave * 16 + i16] = has;
-        // dh of the wave's rows, 32 features at a time in two products: a lane has four of its row's in each, so placed that it
-        // stores sixteen bytes (fp32: 4 q .. 4 q + 3 of either half; bf16: 8 q .. 8 q + 7).  Nothing reads dh soon: past the caches,
-        // where the states wait for their second reading
-        for (int f0 = 0; f0 < H; f0 += 32) {
-            floatx4 d[2] = {{0.0f, 0.0f, 0.0f, 0.0f}, {0.0f, 0.0f, 0.0f, 0.0f}};
+        // dh of the wave's rows, 128 bytes of each at a time: a lane has two pieces of sixteen bytes of its row (fp32: features 4 q ..
+        // 4 q + 3 of either half; bf16: 8 q .. 8 q + 7) and exchanges one with the row eight lanes on, so that a store writes whole
+        // lines of eight rows.  Nothing reads dh soon: past the caches, where the states wait for their second reading
+        constexpr int PER = 16 / (int)sizeof(O), STEP = 8 * PER, D = STEP / 16;
+        const bool low = i16 < 8;
+        const int64_t first = b0 + wave * 16 + (i16 & 7);
+        for (int f0 = 0; f0 < H; f0 += STEP) {
+            floatx4 d[D];
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const int f = f0 + (sizeof(O) == 4 ? u * 16 + i16 : (i16 >> 2) * 8 + u * 4 + (i16 & 3));    // whose weights this lane brings
+            for (int u = 0; u < D; ++u) {
+                d[u] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+                const int f = f0 + (sizeof(O) == 4 ? u * 16 + i16 : (u >> 1) * 32 + (i16 >> 2) * 8 + (u & 1) * 4 + (i16 & 3));    // whose weights this lane brings
                 const int s = f / (4 * V), fq = f / V & 3, e = f % V;
 #pragma unroll
                 for (int ct = 0; ct < CT; ++ct)
@@ -229,25 +233,34 @@ few_backward_kernel(const FewArgs a) {
                     for (int v = 0; v < 4; ++v)
                         d[u] = __builtin_amdgcn_mfma_f32_16x16x4f32(to_f32<T>(table.w[few_at<T>(STEPS, ct, s, fq, q * 4 + v, e)]), g[ct][v], d[u], 0, 0, 0);
             }
-            if (r < a.n) {
-                constexpr int PER = 16 / (int)sizeof(O);
-                O e[8];
+            u32x4 piece[2];
 #pragma unroll
-                for (int k = 0; k < 8; ++k) e[k] = from_f32<O>(has ? d[k >> 2][k & 3] : 0.0f);
+            for (int p = 0; p < 2; ++p) {
+                O e[PER];
 #pragma unroll
-                for (int u = 0; u < 8 / PER; ++u) {
-                    const int f = f0 + u * 16 + q * PER;
-                    O *o = dh + r * H + f;
-                    if (f + PER <= H) {
-                        typedef u32x4 __attribute__((aligned(2))) any4;
-                        u32x4 w;
-                        __builtin_memcpy(&w, e + u * PER, 16);
-                        __builtin_nontemporal_store(w, reinterpret_cast<any4 *>(o));
-                    } else {
+                for (int k = 0; k < PER; ++k) e[k] = from_f32<O>(has ? d[p * (D / 2) + (k >> 2)][k & 3] : 0.0f);
+                __builtin_memcpy(&piece[p], e, 16);
+            }
 #pragma unroll
-                        for (int k = 0; k < PER; ++k)
-                            if (f + k < H) o[k] = e[u * PER + k];
-                    }
+            for (int k = 0; k < 4; ++k) {
+                const uint32_t other = __builtin_amdgcn_mov_dpp(low ? piece[1][k] : piece[0][k], 0x128, 0xF, 0xF, true);      // of lane i16 ^ 8
+                if (low) piece[1][k] = other;
+                else piece[0][k] = other;
+            }
+            const int f = f0 + (low ? 0 : STEP / 2) + q * PER;
+#pragma unroll
+            for (int p = 0; p < 2; ++p) {
+                if (first + 8 * p >= a.n) continue;
+                O *o = dh + (first + 8 * p) * H + f;
+                if (f + PER <= H) {
+                    typedef u32x4 __attribute__((aligned(2))) any4;
+                    __builtin_nontemporal_store(piece[p], reinterpret_cast<any4 *>(o));
+                } else {
+                    O e[PER];
+                    __builtin_memcpy(e, &piece[p], 16);
+#pragma unroll
+                    for (int k = 0; k < PER; ++k)
+                        if (f + k < H) o[k] = e[k];
                 }
             }
         }
