@@ -23,7 +23,7 @@ template <int WM> constexpr int kTN = WM == 5 ? 2 : 4;
 template <int WM> constexpr int kTileT = WM == 4 ? 512 : 256;           // threads
 template <int WM> constexpr int kTileBufs = WM == 4 ? 4 : 3;
 template <int WM> constexpr int kTileBuf = (kTileA<WM> + kTileB) * 64;
-template <int WM> constexpr int kTilePlaces = WM == 4 ? 256 : 512;      // blocks the chip holds at once
+template <int WM> constexpr int kTilePlaces = WM == 4 ? 256 : 512;      // blocks for each of the two products: half of what the chip holds at once
 template <int WM> constexpr int kTileWaves = WM == 4 ? 1 : 2;           // blocks on a CU
 
 // Operands are K-blocked as in operand_offset, in one to three bf16 parts: part p, slab s (32 elements of K), row r
@@ -235,6 +235,7 @@ struct GradArgs {
     void *out;
     float *acc;                     // dV over several chunks of rows
 };
+constexpr uint32_t kLongRange = 1200;      // stages
 constexpr uint32_t kMinStages = 8;       // a range is no shorter
 struct GradPlan {
     uint32_t b_tiles, nk, stages;   // stages of a part product, of a tile
@@ -249,7 +250,12 @@ __device__ __forceinline__ GradPlan grad_plan(const GradArgs &a) {
     g.nk = WEIGHTS ? (rows + 31) / 32 : (a.C + 31) / 32;
     g.stages = g.nk * a.p.pairs.n;
     g.total = g.b_tiles * g.stages;
-    const uint32_t most = grad_ranges(kTilePlaces<WM>, a.a_tiles), per = (g.total + most - 1) / most;
+    // Ranges: dh's and dV's together are as many blocks as the chip holds.  Long ones of several tiles of A are faster one product after
+    // the other, on all of it (both products with joining, bf16 32768 x 512 x 32000 2.15 ms against 2.25; but 16384 rows 1.17 against
+    // 1.15, 8192 x 512 x 16000 305 us against 286, 65536 x 256 x 32000 2.28 ms against 2.16, fp32 3000 x 256 x 8000 194 us against 163).
+    const uint32_t half = grad_ranges(kTilePlaces<WM> / 2, a.a_tiles);
+    const uint32_t most = a.a_tiles > 1 && g.total / half > kLongRange ? grad_ranges(kTilePlaces<WM>, a.a_tiles) : half;
+    const uint32_t per = (g.total + most - 1) / most;
     g.per = per > kMinStages ? per : kMinStages;
     g.ranges = (g.total + g.per - 1) / g.per;
     return g;
