@@ -24,7 +24,9 @@ constexpr int kResT = 256;
 constexpr int kResRows = 256;            // resident rows of a block
 constexpr int kResTile = 32;             // rows of the other operand in a tile
 constexpr int kResBufs = 3;
-constexpr int kResMinTiles = 8;          // a block's range is no shorter
+// A block's range is no shorter; where it makes further rounds of blocks, 8.  (Statistics and g with 8 everywhere and with 2: fp32 2304 x 150
+// x 2003 30 + 43 us, 20 + 25; bf16 2000 x 512 x 2000 21 + 28, 16 + 16; with 2 everywhere fp32 4608 x 150 x 10007 79 + 113, 82 + 136.)
+constexpr int kResMinTiles = 2, kResRoundTiles = 8;
 constexpr int kResBlocks = 1024;         // ranges make no more blocks than this
 constexpr int kResInAcc = 44;            // resident fragments that are kept in accumulation registers, of 64 at most
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
@@ -51,7 +53,7 @@ __host__ __device__ inline int res_ranges(int blocks, int tiles, int places) {
         return fill < most ? fill : most > 1 ? most : 1;
     }
     int best = 1, best_rounds = (blocks + places - 1) / places;
-    for (int s = 2; s <= 32 && blocks * s <= kResBlocks && tiles >= s * kResMinTiles; ++s) {
+    for (int s = 2; s <= 32 && blocks * s <= kResBlocks && tiles >= s * (blocks * s <= places ? kResMinTiles : kResRoundTiles); ++s) {
         const int rounds = (blocks * s + places - 1) / places;
         if (rounds * best * 64 < best_rounds * s * 63) { best = s; best_rounds = rounds; }
     }
