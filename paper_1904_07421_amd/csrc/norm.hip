@@ -5,8 +5,11 @@
 //     xhat = (x - mean) rstd,  y = D(xhat gamma + beta)            D: dropout, where asked for
 // and for a cotangent gy of y, with g = D(gy) and a = g gamma:
 //     dx = rstd (a - sum a / H - xhat sum (a xhat) / H),  dgamma = sum over rows of g xhat,  dbeta = sum over rows of g.
-// A row stays in the registers of the lanes that share it (16 to 64 of a wave, or a block of 512 for long rows) between its two
-// sums and its result, so x is read once and the variance is that of the centred values; everything is fp32.
+// A row stays in the registers of the lanes that share it (16 to 64 of a wave, or a block of 512 for long rows) between its sums and
+// its result, so x is read once and the variance is that of the centred values; everything is fp32.  A mean m0 from a sum in fp32 is
+// off by more than a rounding, which rows far from zero show (30000.1 in every column: by 0.002, and y would be 0.5 instead of beta):
+// what is left of it is the mean of x - m0, summed beside the squares, and comes off both,
+//     c = sum (x - m0) / H,  mean = m0 + c,  sum (x - mean)^2 = sum (x - m0)^2 - c sum (x - m0).
 //
 // Dropout keeps element i of a call (rows one after another) where half i % 2 (low half first) of the 64-bit word
 //     mix64(mix64(seed) + (first + i / 2) golden)                  (SplitMix64 with a mixed key; seed, first: state[0], state[1])
@@ -173,7 +176,7 @@ __device__ __forceinline__ float lanes_sum(float v) {
     for (int m = 1; m < G; m <<= 1) v += __shfl_xor(v, m);
     return v;
 }
-// G <= 64: lanes of a wave.  G = kWide: the block; `red` holds one float per wave, and the caller alternates between two of them.
+// G <= 64: lanes of a wave.  G = kWide: the block; `red` holds one float per wave, and two sums in a row need two of them.
 template <int G>
 __device__ __forceinline__ float row_sum(float v, float *red) {
     if constexpr (G <= 64) {
@@ -186,6 +189,26 @@ __device__ __forceinline__ float row_sum(float v, float *red) {
 #pragma unroll
         for (int w = 0; w < G / 64; ++w) s += red[w];
         return s;
+    }
+}
+
+// two at once; `red` holds two floats per wave
+template <int G>
+__device__ __forceinline__ void row_sums(float &v, float &w, float *red) {
+    v = lanes_sum<(G <= 64 ? G : 64)>(v);
+    w = lanes_sum<(G <= 64 ? G : 64)>(w);
+    if constexpr (G > 64) {
+        if ((threadIdx.x & 63) == 0) {
+            red[threadIdx.x >> 6] = v;
+            red[G / 64 + (threadIdx.x >> 6)] = w;
+        }
+        __syncthreads();
+        v = w = 0.0f;
+#pragma unroll
+        for (int k = 0; k < G / 64; ++k) {
+            v += red[k];
+            w += red[G / 64 + k];
+        }
     }
 }
 
@@ -207,7 +230,7 @@ template <typename T, int G, int NV>
 __global__ void __launch_bounds__(G <= 64 ? kT : kWide)
 layernorm_kernel(const NormArgs a) {
     constexpr int V = kVec<T>, THREADS = G <= 64 ? kT : kWide, GROUPS = THREADS / G;
-    __shared__ float red[G <= 64 ? 1 : 2 * kWide / 64];
+    __shared__ float red[G <= 64 ? 1 : 3 * kWide / 64];
     const int l = threadIdx.x % G, H = a.H;
     const T *x = static_cast<const T *>(a.x);
     const uint64_t start = a.drop.state ? drop_start(a.drop) : 0;
@@ -244,22 +267,27 @@ layernorm_kernel(const NormArgs a) {
 #pragma unroll
             for (int k = 0; k < V; ++k) s += v[j][k];
         }
-        const float mean = row_sum<G>(s, red) / (float)H;         // a quotient: the mean of equal values is that value
-        s = 0.0f;
+        const float m0 = row_sum<G>(s, red) / (float)H;           // (a quotient: a product would be fused into the differences, unrounded)
+        float off = 0.0f, sq = 0.0f;
 #pragma unroll
         for (int j = 0; j < NV; ++j)
 #pragma unroll
             for (int k = 0; k < V; ++k) {
-                v[j][k] -= mean;
-                if ((j * G + l) * V + k < H) s += v[j][k] * v[j][k];
+                v[j][k] -= m0;
+                if ((j * G + l) * V + k < H) {
+                    off += v[j][k];
+                    sq += v[j][k] * v[j][k];
+                }
             }
-        const float rstd = 1.0f / sqrtf(row_sum<G>(s, red + kWide / 64 * (G > 64)) * a.inv_h + a.eps);
+        row_sums<G>(off, sq, red + kWide / 64 * (G > 64));
+        const float more = off * a.inv_h, mean = more == more ? m0 + more : m0, left = sq - off * more;       // (an infinite mean stays one)
+        const float rstd = 1.0f / sqrtf((left < 0.0f ? 0.0f : left) * a.inv_h + a.eps);        // (below 0 by rounding alone: equal values)
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             const int c = (j * G + l) * V;
             if (c >= H) continue;
 #pragma unroll
-            for (int k = 0; k < V; ++k) v[j][k] = v[j][k] * rstd * gamma[j][k] + beta[j][k];
+            for (int k = 0; k < V; ++k) v[j][k] = (v[j][k] - more) * rstd * gamma[j][k] + beta[j][k];
             if (a.drop.state) apply_drop<V>(a.drop, start, (uint64_t)row * H + c, v[j]);
             store_row_piece<T, V>(static_cast<T *>(a.y) + row * H + c, H - c, v[j]);
         }

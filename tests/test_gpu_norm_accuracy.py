@@ -1,0 +1,71 @@
+"""Layer norm of rows that lie far from zero: what is left of an fp32 mean comes off as well."""
+import numpy as np
+import pytest
+
+from oracle import head_oracle as O
+
+pytestmark = pytest.mark.gpu
+
+U32 = 2.0 ** -24                         # half a step of fp32, relative
+WIDTHS = [3, 150, 203, 300, 513, 2048, 2049, 5000]
+
+
+def _norm(x, gamma, beta, eps=1e-5):
+    import torch
+    import paper_1904_07421_amd as J
+    to = lambda a: torch.from_numpy(np.ascontiguousarray(a, dtype=np.float32)).cuda()  # noqa: E731
+    return [t.cpu().numpy().astype(np.float64) for t in J.jitdb_layernorm_forward(to(x), to(gamma), to(beta), eps=eps)]
+
+
+def _depth(H):
+    """Additions in a row of a sum of H values: at most 32 of a lane, then a tree over lanes and waves."""
+    return 34 + np.ceil(np.log2(H + 1))
+
+
+@pytest.mark.parametrize("H", WIDTHS)
+def test_rows_of_equal_values(H):
+    """mean is the value itself; x - mean is what an fp32 correction of at most depth 2^-24 |x| may itself be off by."""
+    values = np.array([0.1, -0.3, 7.25, 1e-20, 30000.1, 100000.1, -3.3e6, 1e15], np.float32)
+    x = np.repeat(values[:, None], H, 1)
+    gamma, beta = np.full(H, 1.5), np.full(H, 0.25)
+    y, mean, rstd = _norm(x, gamma, beta)
+    assert np.array_equal(mean, values.astype(np.float64))
+    off = ((_depth(H) + 1) * U32) ** 2 * np.abs(values.astype(np.float64))      # of the correction of the correction
+    assert np.all(np.abs(y - 0.25) <= (1.5 * off / np.sqrt(1e-5))[:, None] * (1 + 1e-3) + 2 * U32)
+    # the variance is 0 up to the rounding of (what was corrected)^2
+    d2 = ((_depth(H) + 1) * U32 * np.abs(values.astype(np.float64))) ** 2
+    assert np.all(np.abs(rstd * np.sqrt(1e-5) - 1) <= (2 * _depth(H) + 4) * U32 * d2 / 1e-5 + 4 * U32)
+
+
+@pytest.mark.parametrize("H", WIDTHS)
+@pytest.mark.parametrize("far", [0.0, 1e2, 1e4, -1e5])
+def test_rows_far_from_zero(H, far):
+    rng = np.random.default_rng([H, int(abs(far))])
+    x = (far + rng.standard_normal((40, H))).astype(np.float32)
+    gamma, beta = (rng.standard_normal(H).astype(np.float32) for _ in range(2))
+    y_t, mean_t, rstd_t = _norm(x, gamma, beta)
+    x = x.astype(np.float64)
+    y, mean, rstd = O.layernorm(x, gamma.astype(np.float64), beta.astype(np.float64), 1e-5)
+    k = _depth(H) + 2
+    first = k * U32 * np.abs(x).mean(1, keepdims=True)              # what the first mean may be off by
+    d = np.abs(x - mean[:, None]) + first                           # the values that are summed, corrected and scaled
+    corr = k * U32 * d.mean(1, keepdims=True)                       # error of the correction: its sum, the product with 1 / H
+    assert np.all(np.abs(mean_t - mean)[:, None] <= corr * (1 + U32) + U32 * np.abs(mean)[:, None])
+    d_err = corr + 2 * U32 * d                                      # both differences rounded
+    # squares and what comes off them, each a sum of that depth, and twice the correction's error times what it multiplies
+    var_err = (2 * k * U32 * (d ** 2).mean(1, keepdims=True) + 2 * first * corr)
+    rstd_rel = 0.5 * var_err * rstd[:, None] ** 2 * (1 + 1e-3) + 4 * U32
+    assert np.all(np.abs(rstd_t / rstd - 1)[:, None] <= rstd_rel)
+    bound = np.abs(gamma) * rstd[:, None] * (d_err + d * (rstd_rel + 3 * U32)) + 4 * U32 * (np.abs(y) + np.abs(beta))
+    assert np.all(np.abs(y_t - y) <= bound)
+
+
+def test_rows_that_are_not_finite():
+    import torch
+    import paper_1904_07421_amd as J
+    x = torch.randn(4, 203, device="cuda")
+    x[0, 7], x[1, 9], x[2, 11] = float("inf"), -float("inf"), float("nan")
+    one = torch.ones(203, device="cuda")
+    y, mean, _ = J.jitdb_layernorm_forward(x, one, one)
+    assert float(mean[0]) == float("inf") and float(mean[1]) == -float("inf") and bool(mean[2].isnan())
+    assert bool(y[:3].isnan().any(1).all()) and bool(y[3].isfinite().all())
