@@ -29,7 +29,7 @@ constexpr int kResBufs = 3;
 constexpr int kResMinTiles = 2, kResRoundTiles = 8;
 constexpr int kResBlocks = 1024;         // ranges make no more blocks than this
 constexpr int kResInAcc = 44;            // resident fragments that are kept in accumulation registers, of 64 at most
-constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f, kLn2Low = (float)(0.69314718055994530942 - (double)kLn2);
 
 struct ResArgs {
     const char *res; int64_t res_slab;   // the resident operand, K-blocked, the parts' slabs behind one another
@@ -68,11 +68,13 @@ __device__ __forceinline__ void static_for_impl(F &&f, std::integer_sequence<int
 template <int N, typename F>
 __device__ __forceinline__ void static_for(F &&f) { static_for_impl(f, std::make_integer_sequence<int, N>()); }
 
-// e^x: the hardware's 2^t, corrected for the rounding of t = x log2 e.  (Not of -inf itself, whose correction would be NaN.)
+// e^x: the hardware's 2^t, good to a unit in the last place, with t = x log2 e rounded, times 1 + c, c = x - t ln 2: what the rounding
+// of t and of log2 e itself left out.  ln 2 in two words: of one, t 1.9e-9 would stay, always in the same direction (as the lower word
+// of log2 e did while c was computed from the upper: 2.3e-7 at -17, 1.2e-6 at -80).  (Not of -inf itself, whose c would be NaN.)
 __device__ __forceinline__ float exp_close(float x) {
     x = x < -200.0f ? -200.0f : x;
     const float t = x * kLog2e, p = __builtin_amdgcn_exp2f(t);
-    return fmaf(p, kLn2 * fmaf(x, kLog2e, -t), p);
+    return fmaf(p, fmaf(-t, kLn2Low, fmaf(-t, kLn2, x)), p);
 }
 
 // A read of LDS that the compiler does not wait for: it would make it wait for every direct-to-LDS load in flight.
@@ -108,7 +110,7 @@ resident_kernel(const ResArgs a) {
     constexpr int EARLY = (NG - 3) * 2;                  // fragments
     constexpr int SLOTS = G == 0 || !res_alone(NF, G > 0) ? PRODUCTS : res_products<PARTS>(EARLY);
     constexpr bool ALONE = res_alone(NF, G > 0);
-    constexpr bool CLOSE = PARTS == 3 || G == 3;         // fp32 results: exponentials good to a rounding
+    constexpr bool CLOSE = PARTS == 3 || G == 3;         // fp32 results: exponentials good to two roundings
     __shared__ __attribute__((aligned(1024))) char lds[kResBufs * BUF];
     const int left = *a.n_rows - a.row0, rows = left < 0 ? 0 : left < a.max_rows ? left : a.max_rows;
     const int blocks = G == 0 ? (rows + kResRows - 1) / kResRows : a.class_blocks;
