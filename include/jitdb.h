@@ -487,7 +487,8 @@ int jitdb_layernorm_backward(const void *x, const float *gamma, const float *mea
  *
  *   h        dev [n_rows, H] in dtype elements
  *   V        dev [n_classes, H] in dtype elements
- *   b        dev [n_classes] fp32 or NULL (= zeros); -inf takes a class out
+ *   b        dev [n_classes] fp32 or NULL (= zeros); -inf takes a class out.  A logit of +inf makes lse +inf, and the loss +inf or,
+ *            where it is the label's own, NaN
  *   label    dev [n_rows] int32.  -1: the row has no label; it is not multiplied, its loss and lse are 0 and
  *            its gradient is 0, whatever h holds there.  Any other value outside [0, n_classes): the row's loss,
  *            and with it the gradients it has a part in, are NaN.

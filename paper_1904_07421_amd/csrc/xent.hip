@@ -264,7 +264,7 @@ join_kernel(const JoinArgs a) {
     auto add = [&](float2 p) {
         if (p.y == 0.0f) return;                     // nothing but masked classes
         const float m = fmaxf(top, p.x);
-        s = s * expf(top - m) + p.y * expf(p.x - m);
+        s = s * exp_below(top, m) + p.y * exp_below(p.x, m);
         top = m;
     };
     if (r < rows)

@@ -146,7 +146,7 @@ few_forward_kernel(const FewArgs a) {
                     if (label == ct * 16 + q * 4 + v) at = z[ct][v];
                 }
             top = quarters_max(top);
-            const float from = top == -INFINITY ? 0.0f : top;       // every class masked: the sum is 0, not NaN
+            const float from = fabsf(top) == INFINITY ? 0.0f : top;       // every class masked: the sum is 0, not NaN; a logit of +inf: it is +inf
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct)
 #pragma unroll

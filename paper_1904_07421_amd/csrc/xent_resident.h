@@ -77,6 +77,9 @@ __device__ __forceinline__ float exp_close(float x) {
     return fmaf(p, fmaf(-t, kLn2Low, fmaf(-t, kLn2, x)), p);
 }
 
+// e^(x - top) for a largest x of `top`: of +inf only the largest themselves count (inf - inf is no number)
+__device__ __forceinline__ float exp_below(float x, float top) { return x == INFINITY ? 1.0f : expf(x - top); }
+
 // A read of LDS that the compiler does not wait for: it would make it wait for every direct-to-LDS load in flight.
 template <int OFFSET>
 __device__ __forceinline__ void lds_read16(u32x4 &to, uint32_t at) { asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(to) : "v"(at), "n"(OFFSET) : "memory"); }
@@ -260,9 +263,9 @@ resident_kernel(const ResArgs a) {
 #pragma unroll
                 for (int v = 0; v < 16; ++v) m = fmaxf(m, z[j][v]);
                 const float from = m == -INFINITY ? 0.0f : m;            // nothing but masked classes so far
-                float again = kept[j] * expf(ref[j] - from);
+                float again = kept[j] * exp_below(ref[j], from);
 #pragma unroll
-                for (int v = 0; v < 16; ++v) again += expf(z[j][v] - from);
+                for (int v = 0; v < 16; ++v) again += exp_below(z[j][v], from);
                 sum[j] = out ? again : sum[j];
                 ref[j] = out ? m : ref[j];                               // (stays -inf until a class is not masked)
                 ref_l[j] = ref[j] * kLog2e;
@@ -465,7 +468,7 @@ resident_kernel(const ResArgs a) {
 #pragma unroll
         for (int j = 0; j < 2; ++j) {        // the two lanes of a row
             const float ref2 = __shfl_xor(ref[j], 32), sum2 = __shfl_xor(kept[j], 32), top = fmaxf(ref[j], ref2), m = top == -INFINITY ? 0.0f : top;
-            const float s = kept[j] * expf(ref[j] - m) + sum2 * expf(ref2 - m);
+            const float s = kept[j] * exp_below(ref[j], m) + sum2 * exp_below(ref2, m);
             if (hf == 0) a.stat[((int64_t)range * blocks + rb) * kResRows + wave * 64 + j * 32 + l32] = make_float2(m, s);
         }
     } else {

@@ -445,6 +445,14 @@ wide_logits_kernel(const LogitArgs a) {
             for (int t = 0; t < 2; ++t)
 #pragma unroll
                 for (int v = 0; v < 16; ++v) s += CLOSE ? exp_close(acc[t][j][v] - from) : __expf(acc[t][j][v] - from);
+            if (top == INFINITY) {                                  // (inf - inf is no number)
+                s = 1.0f;
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v)
+                        if (acc[t][j][v] != acc[t][j][v]) s = acc[t][j][v];
+            }
             s += __shfl_xor(s, 32);
             if (hf == 0) a.stat[(int64_t)(2 * ct + wm) * a.max_rows + r] = make_float2(from, s);
         }

@@ -18,3 +18,46 @@ def test_probabilities_far_below_one(dtype, H, C):
     _, _, db = J.jitdb_softmax_xent_backward(h, V, torch.zeros(1, dtype=torch.int32, device="cuda"), torch.zeros(1, device="cuda"), b=b)
     got, want = db.double().cpu().numpy()[1:], np.exp(b.double().cpu().numpy())[1:]
     assert np.abs(got / want - 1).max() <= 2.0 ** -23 + 2.0 ** -24 + 2.0 ** -26
+
+
+SHAPES = [("f32", 40, 5), ("f32", 700, 20), ("bf16", 512, 64), ("f32", 150, 1000), ("f32", 200, 400), ("bf16", 256, 1000), ("bf16", 512, 5000),
+          ("bf16", 600, 400)]             # few classes, resident operands, both operands streaming
+
+
+@pytest.mark.parametrize("dtype,H,C", SHAPES)
+@pytest.mark.parametrize("n", [3, 300])
+def test_a_logit_of_plus_infinity(n, dtype, H, C):
+    """log-sum-exp is +inf, and so is the loss of every other label; a NaN beside it stays one."""
+    import torch
+    import paper_1904_07421_amd as J
+    print(f"xent +inf n={n} H={H} C={C} {dtype}", flush=True)
+    dt = torch.float32 if dtype == "f32" else torch.bfloat16
+    torch.manual_seed(C)
+    h, V = torch.randn(n, H, device="cuda").to(dt), torch.randn(C, H, device="cuda").to(dt)
+    for where in ([0], [C // 2], [C - 1], [0, 1, C - 1]):
+        b = torch.randn(C, device="cuda")
+        b[2] = -float("inf")
+        b[where] = float("inf")
+        label = torch.full((n,), 3, dtype=torch.int32, device="cuda")
+        label[1] = where[0]
+        loss, lse = J.jitdb_softmax_xent_forward(h, V, label, b=b)
+        want = torch.full((n,), float("inf"), device="cuda")
+        assert torch.equal(lse, want), where
+        assert bool(loss[1].isnan()) and torch.equal(loss[[0, *range(2, n)]], want[1:])
+        b[C // 3] = float("nan")
+        loss, lse = J.jitdb_softmax_xent_forward(h, V, label, b=b)
+        assert bool(lse.isnan().all()) and bool(loss.isnan().all())
+
+
+@pytest.mark.parametrize("dtype,H,C", SHAPES)
+def test_every_class_behind_minus_infinity(dtype, H, C):
+    """No class is left: log-sum-exp is -inf, and the loss has no value."""
+    import torch
+    import paper_1904_07421_amd as J
+    dt = torch.float32 if dtype == "f32" else torch.bfloat16
+    h, V = torch.randn(70, H, device="cuda").to(dt), torch.randn(C, H, device="cuda").to(dt)
+    label = torch.full((70,), C - 1, dtype=torch.int32, device="cuda")
+    label[5] = -1
+    loss, lse = J.jitdb_softmax_xent_forward(h, V, label, b=torch.full((C,), -float("inf"), device="cuda"))
+    rest = torch.arange(70, device="cuda") != 5
+    assert bool((lse[rest] == -float("inf")).all()) and bool(loss[rest].isnan().all()) and float(lse[5]) == float(loss[5]) == 0
