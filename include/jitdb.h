@@ -486,7 +486,8 @@ int jitdb_layernorm_backward(const void *x, const float *gamma, const float *mea
  *     z_nc = <h_n, V_c> + b_c      lse_n = log sum_c exp(z_nc)      loss_n = lse_n - z_n,label(n)
  *
  *   h        dev [n_rows, H] in dtype elements
- *   V        dev [n_classes, H] in dtype elements
+ *   V        dev [n_classes, H] in dtype elements.  Values of h (in rows with a label), V and gloss are to be finite: what one that is
+ *            not has a part in is NaN or infinite (NaN for fp32 operands of many classes, which are multiplied in parts)
  *   b        dev [n_classes] fp32 or NULL (= zeros); -inf takes a class out.  A logit of +inf makes lse +inf, and the loss +inf or,
  *            where it is the label's own, NaN
  *   label    dev [n_rows] int32.  -1: the row has no label; it is not multiplied, its loss and lse are 0 and

@@ -24,6 +24,7 @@ namespace jitdb {
 namespace {
 
 constexpr int kMaxClasses = 1 << 22;
+constexpr float kMaxBf16 = 0x1.FEp127f;
 constexpr int kMaxWidth = 1 << 14;
 constexpr int kLabelBlock = 1024, kLabelBlocks = 2048;     // labels of a block of the listing kernels at least, most blocks of them
 constexpr int64_t kStatBytes = 512ll << 20;   // of tile statistics of wide states kept at once (forward) ...
@@ -99,7 +100,8 @@ label_rows_kernel(const RowList a) {
 }
 
 // ---- packing ---------------------------------------------------------------------------------------
-// bf16 parts of eight values: v = sum of parts, exactly for three of them (down to the smallest bf16)
+// bf16 parts of eight values: v = sum of parts, exactly for three of them (down to the smallest bf16).  The first is held at the largest
+// bf16, which fp32 goes beyond by up to half its step.
 template <typename T, int PARTS>
 __device__ __forceinline__ void store_parts(const T (&e)[8], char *to, int64_t part) {
     if constexpr (sizeof(T) == 2) {
@@ -113,7 +115,8 @@ __device__ __forceinline__ void store_parts(const T (&e)[8], char *to, int64_t p
             u32x4 w;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                w[j] = pack_bf16(v[2 * j], v[2 * j + 1]);
+                if (i == 0) w[j] = pack_bf16(__builtin_amdgcn_fmed3f(v[2 * j], -kMaxBf16, kMaxBf16), __builtin_amdgcn_fmed3f(v[2 * j + 1], -kMaxBf16, kMaxBf16));
+                else w[j] = pack_bf16(v[2 * j], v[2 * j + 1]);
                 v[2 * j] -= low_bf16(w[j]);
                 v[2 * j + 1] -= high_bf16(w[j]);
             }

@@ -61,3 +61,30 @@ def test_every_class_behind_minus_infinity(dtype, H, C):
     loss, lse = J.jitdb_softmax_xent_forward(h, V, label, b=torch.full((C,), -float("inf"), device="cuda"))
     rest = torch.arange(70, device="cuda") != 5
     assert bool((lse[rest] == -float("inf")).all()) and bool(loss[rest].isnan().all()) and float(lse[5]) == float(loss[5]) == 0
+
+
+@pytest.mark.parametrize("C", [20, 100, 700])
+@pytest.mark.parametrize("H", [4, 150, 200])
+def test_fp32_values_above_the_largest_bf16(H, C):
+    """The largest fp32 values, times class weights that bring them back: logits up to 60."""
+    import torch
+    import paper_1904_07421_amd as J
+    from oracle import head_oracle as O
+    from test_gpu_xent import _f32, _host, _i32, _tolerances
+    print(f"xent largest values H={H} C={C}", flush=True)
+    n = 6
+    rng = np.random.default_rng([H, C])
+    h, V = np.zeros((n, H), np.float32), np.zeros((C, H), np.float32)
+    big = (2 - 2.0 ** -23) * 2.0 ** 127
+    h[:4, H // 2] = big, -big, (2 - 2.0 ** -8) * 2.0 ** 127, (2 - 2.0 ** -7) * 2.0 ** 127      # ... half a step above the largest bf16, it itself
+    h[4:] = rng.uniform(-1, 1, (2, H))
+    V[:, H // 2] = (np.arange(C) % 16) * 2.0 ** -126
+    label, gloss = rng.integers(0, C, n), rng.uniform(0.1, 0.4, n).astype(np.float32)
+    loss_t, lse_t = J.jitdb_softmax_xent_forward(_f32(h), _f32(V), _i32(label))
+    dh_t, dV_t, db_t = J.jitdb_softmax_xent_backward(_f32(h), _f32(V), _i32(label), lse_t, gloss=_f32(gloss))
+    h, V = h.astype(np.float64), V.astype(np.float64)
+    loss, lse = O.softmax_xent(h, V, None, label)
+    dh, dV, db, g, p = O.softmax_xent_backward(h, V, None, label, gloss.astype(np.float64))
+    loss_err, lse_err, dh_err, dV_err, db_err, out = _tolerances(h, V, None, label, gloss, "f32", "f32", loss, lse, g, p)
+    for t, want, err in ((loss_t, loss, loss_err), (lse_t, lse, lse_err), (db_t, db, db_err), (dV_t, dV, dV_err), (dh_t, dh, dh_err)):
+        assert np.all(np.abs(_host(t) - want) <= err * (1 + out) + out * np.abs(want) + 1e-36)
