@@ -8,6 +8,7 @@
 #include <new>
 
 #include "jitdb.h"
+#include "rounding.h"
 
 namespace jitdb {
 
@@ -25,9 +26,6 @@ struct Carver {
         return p;
     }
 };
-
-inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
-inline int64_t round_up(int64_t a, int64_t b) { return ceil_div(a, b) * b; }
 
 // Where and why the last JITDB_E_HIP happened (process-wide, for diagnostics only).
 void note_hip_failure(hipError_t e, const char *file, int line);

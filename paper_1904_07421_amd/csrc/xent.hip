@@ -23,12 +23,7 @@
 namespace jitdb {
 namespace {
 
-constexpr int kMaxClasses = 1 << 22;
 constexpr float kMaxBf16 = 0x1.FEp127f;
-constexpr int kMaxWidth = 1 << 14;
-constexpr int kLabelBlock = 1024, kLabelBlocks = 2048;     // labels of a block of the listing kernels at least, most blocks of them
-constexpr int64_t kStatBytes = 512ll << 20;   // of tile statistics of wide states kept at once (forward) ...
-constexpr int64_t kGradBytes = 4ll << 30;     // ... and of g (backward): rows beyond come in further chunks
 
 // ---- the labelled rows -----------------------------------------------------------------------------
 struct RowList {
@@ -289,67 +284,7 @@ clear_kernel(O *__restrict__ p, int64_t n) {
     for (int64_t i = (int64_t)blockIdx.x * kT + threadIdx.x; i < n; i += (int64_t)gridDim.x * kT) p[i] = O(0);
 }
 
-// ---- sizes and workspaces ------------------------------------------------------------------------------
-struct Sizes {
-    int64_t n, n_pad;          // rows at most, and rounded up to whole tiles
-    int H, C, Hk, Hf, Cp;      // widths: of K (states), of the turned states' rows, classes in whole tiles
-    int wm, tile_a, a_tiles, places;      // of the gradients' products: variant, features of a tile, tiles, blocks on the chip
-    int parts, g_parts;        // of the operands, of g
-    int label_per, label_blocks;
-    int res, class_tiles;      // resident_kernel: K in steps of 16 (0: not for this width), tiles of 32 classes
-    int stat_rows, grad_rows;  // rows of a chunk
-};
-bool known(jitdb_dtype t) { return t == JITDB_F32 || t == JITDB_BF16; }
-// K in steps of 16 of the variant of resident_kernel for this width: the fragments of 64 rows in up to 256 registers.  (bf16 32768 x 512
-// x 50021: statistics 1.48 ms, g 1.83; with both operands streaming, as wider states have them, 1.78 and 2.83.)
-int res_steps(int H, jitdb_dtype dtype) {
-    if (dtype == JITDB_F32) return H <= 128 ? 8 : H <= 160 ? 10 : 0;
-    return H <= 128 ? 8 : H <= 256 ? 16 : H <= 384 ? 24 : H <= 512 ? 32 : 0;
-}
-bool make_sizes(int64_t n, int32_t H, int32_t C, jitdb_dtype dtype, jitdb_dtype grad, Sizes &s) {
-    if (n < 0 || n > JITDB_MAX_NODES || H < 1 || H > kMaxWidth || C < 1 || C > kMaxClasses || !known(dtype) || !known(grad)) return false;
-    if (dtype == JITDB_F32 && grad == JITDB_BF16) return false;       // gradients are not rounded below their operands
-    s.n = n; s.H = H; s.C = C;
-    s.n_pad = round_up(n > 0 ? n : 1, 256);
-    s.res = res_steps(H, dtype);
-    s.Hk = s.res ? s.res * 16 : (int)round_up(H, 32);
-    // The tile height that pads the features least, of equals the highest.  Both gradients' products: bf16 65536 x 150 x 32000 in tiles of
-    // 160 features 1.70 ms, of 256 2.18; fp32 30000 x 300 x 8000 of 160 2.08, of 128 2.34; 30000 x 450 x 8000 of 160 3.21, of 256 3.32.
-    auto take_tile = [&](auto wm) {
-        constexpr int WM = decltype(wm)::value, A = kTileA<WM>;
-        if (s.wm && round_up(H, A) >= (int64_t)s.tile_a * s.a_tiles) return;
-        s.wm = WM; s.tile_a = A; s.a_tiles = (int)ceil_div(H, A); s.places = kTilePlaces<WM>;
-    };
-    s.wm = 0;
-    take_tile(std::integral_constant<int, 4>());
-    take_tile(std::integral_constant<int, 5>());
-    take_tile(std::integral_constant<int, 2>());
-    s.Hf = (int)round_up((int64_t)s.tile_a * s.a_tiles, 64);
-    s.Cp = (int)round_up(C, 256);
-    s.class_tiles = (int)ceil_div(C, kResTile);
-    s.parts = dtype == JITDB_F32 ? 3 : 1;
-    s.g_parts = grad == JITDB_F32 ? 3 : 1;
-    s.label_per = kLabelBlock * (int)ceil_div(n > 0 ? n : 1, (int64_t)kLabelBlock * kLabelBlocks);
-    s.label_blocks = (int)ceil_div(n > 0 ? n : 1, s.label_per);
-    auto chunk = [&](int64_t bytes_a_row, int64_t budget) {
-        const int64_t rows = budget / bytes_a_row / 256 * 256;
-        return (int)(rows < 256 ? 256 : rows < s.n_pad ? rows : s.n_pad);
-    };
-    s.stat_rows = s.res ? (int)s.n_pad : chunk((int64_t)s.Cp / 64 * 8, kStatBytes);
-    s.grad_rows = chunk((int64_t)s.Cp * 2 * s.g_parts, kGradBytes);
-    return true;
-}
-// most blocks of resident_kernel with at most `blocks` blocks of resident rows and `tiles` tiles to walk over (res_ranges)
-int64_t res_most(int64_t blocks, int64_t tiles) {
-    const int64_t ranges = tiles / kResMinTiles > 1 ? tiles / kResMinTiles : 1, most = blocks > kResBlocks ? blocks : kResBlocks;
-    return blocks * ranges < most ? blocks * ranges : most;
-}
-// most shares of tiles (grad_plan): of every tile of A, a tile of B more than ranges
-int64_t grad_parts(const Sizes &s, int64_t b_tiles, int64_t nk, int pairs) {
-    const int64_t most = grad_ranges(s.places, s.a_tiles), ranges = ceil_div(b_tiles * nk * pairs, kMinStages);
-    return s.a_tiles * (b_tiles + (ranges < most ? ranges : most));
-}
-int pair_count(int a, int b) { return a == 3 && b == 3 ? 6 : a * b; }        // (one part and three: three products)
+// ---- workspaces ----------------------------------------------------------------------------------------
 struct Space {
     int32_t *counts, *n_rows, *row_of, *label_of;
     float *side, *label_z, *bias, *db_part, *part_h, *part_v, *acc_v;
@@ -435,11 +370,9 @@ int launch_resident(int steps, int64_t blocks, const ResArgs &a, hipStream_t st)
     return JITDB_OK;
 }
 
-// `sets` of statistics, if every row has a label: many take sixteen waves (800 rows, 938 sets: 141 -> 52 us), few four (4608 rows, 28 sets:
-// 14 -> 8 us)
-int launch_join(const JoinArgs &a, int sets, int64_t rows, hipStream_t st) {
+int launch_join(const JoinArgs &a, const Sizes &s, int64_t rows, hipStream_t st) {
     const unsigned blocks = (unsigned)ceil_div(rows, 64);
-    if (sets > 64) join_kernel<16><<<blocks, 64 * 16, 0, st>>>(a);
+    if (join_waves(stat_sets(s)) == 16) join_kernel<16><<<blocks, 64 * 16, 0, st>>>(a);
     else join_kernel<4><<<blocks, 64 * 4, 0, st>>>(a);
     JITDB_LAUNCH_CHECK();
     return JITDB_OK;
@@ -457,12 +390,12 @@ int run_forward_xent(const T *h, const T *V, const float *b, const RowList &list
         a.n_rows = w.n_rows; a.max_rows = (int)s.n_pad; a.class_tiles = s.class_tiles; a.stat = w.stat;
         if ((rc = launch_resident<T, 0>(s.res, res_most(s.n_pad / kResRows, s.class_tiles), a, st)) != JITDB_OK) return rc;
         j.class_tiles = s.class_tiles; j.places = res_places(s.parts * s.res, false); j.max_rows = a.max_rows;
-        return launch_join(j, res_ranges((int)(s.n_pad / kResRows), j.class_tiles, j.places), s.n, st);
+        return launch_join(j, s, s.n, st);
     }
     LogitArgs a = {};
     a.p.A = w.v; a.p.B = w.h; a.p.pairs = make_pairs(s.parts, s.parts);
     a.nk = s.Hk / 32; a.a_tiles = s.Cp / 128; a.n_rows = w.n_rows; a.bias = w.bias; a.stat = w.stat;
-    a.max_rows = j.max_rows = s.stat_rows; j.n_stat = 2 * a.a_tiles;
+    a.max_rows = j.max_rows = s.stat_rows; j.n_stat = stat_sets(s);
     for (int64_t r0 = 0; r0 < s.n; r0 += s.stat_rows) {
         a.row0 = (int)r0;
         a.p.B.at = w.h.at + r0 * 64;
@@ -470,7 +403,7 @@ int run_forward_xent(const T *h, const T *V, const float *b, const RowList &list
         wide_logits_kernel<0, sizeof(T) == 4><<<xcd_grid(ceil_div(rows, 256) * a.a_tiles), kTileT<2>, 0, st>>>(a);
         JITDB_LAUNCH_CHECK();
         j.row0 = a.row0;
-        if ((rc = launch_join(j, j.n_stat, rows, st)) != JITDB_OK) return rc;
+        if ((rc = launch_join(j, s, rows, st)) != JITDB_OK) return rc;
     }
     return JITDB_OK;
 }
@@ -529,11 +462,6 @@ int run_backward_xent(const T *h, const T *V, const float *b, const RowList &lis
 }
 
 // ---- few classes ---------------------------------------------------------------------------------------
-// Is there a variant for these sizes?
-bool few_fits(int H, int C, jitdb_dtype dtype) {
-    auto any = [](auto, auto) {};
-    return dtype == JITDB_F32 ? for_few<float>(H, C, any) : for_few<bf16_t>(H, C, any);
-}
 // Of the backward pass, each of which leaves a set of sums.  A single block writes the gradients itself, a launch less (62 rows of 160,
 // 5 classes, fp32: 12.1 -> 10.3 us in a graph; two turns of a single block lose: 128 rows 16.6 us, with two blocks 12.1).
 int few_blocks(int64_t n) {

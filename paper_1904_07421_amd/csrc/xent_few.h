@@ -11,12 +11,12 @@
 #pragma once
 
 #include "level_common.h"
+#include "xent_sizes.h"
 
 namespace jitdb {
 namespace {
 
 constexpr int kFewT = 256;               // threads of a block: four waves
-constexpr int kFewRows = 64;             // rows a block works on at once
 template <typename T> constexpr int kFewVec = 16 / (int)sizeof(T);        // elements of one load
 template <typename T> constexpr int kFewBlock = 64 * kFewVec<T>;          // features that four waves cover with one load a lane
 
@@ -348,29 +348,27 @@ few_reduce_kernel(const float *__restrict__ part, int n_parts, int H, int C, O *
     else db[c - weights] = s;
 }
 
-// The variant of H features and C classes: launch(classes / 16, blocks of features), false where the weights do not fit LDS with the rest:
-// taken wherever it fits (forward and backward of 100 k rows, the last size that fits and the next: fp32 150 x 64 218 us, 150 x 65 720;
-// 512 x 32 323, 512 x 48 1247; bf16 512 x 64 444, 512 x 65 606).
+// The variant of H features and C classes: launch(classes / 16, blocks of features), false where there is none.
 template <typename T, typename F>
 bool for_few(int H, int C, F &&launch) {
-    const int nb = (int)ceil_div(H, kFewBlock<T>), ct = (int)ceil_div(C, 16);
+    const FewSizes few = few_sizes(sizeof(T), H, C);
     auto with = [&](auto c, auto b) {
         constexpr int CT = decltype(c)::value, NB = decltype(b)::value;
-        // 128 registers of sums a lane; weights and two sets of g in LDS
-        if constexpr (CT * NB * kFewVec<T> <= 32 && sizeof(FewTable<T, CT, NB>) + 2 * kFewRows * (CT * 64 + 4) <= 160 * 1024) { launch(c, b); return true; }
-        return false;
+        static_assert(sizeof(FewTable<T, CT, NB>) == few_table_bytes(CT, NB), "what the rule counts with is what there is");
+        if constexpr (few_variant(sizeof(T), CT, NB)) {
+            if (few.ct == CT && few.nb == NB) launch(c, b);
+        }
     };
     auto blocks = [&](auto c) {
-        if (nb <= 1) return with(c, std::integral_constant<int, 1>());
-        if (nb <= 2) return with(c, std::integral_constant<int, 2>());
-        if (nb <= 4) return with(c, std::integral_constant<int, 4>());
-        if (nb <= 8) return with(c, std::integral_constant<int, 8>());
-        return false;
+        with(c, std::integral_constant<int, 1>());
+        with(c, std::integral_constant<int, 2>());
+        with(c, std::integral_constant<int, 4>());
+        with(c, std::integral_constant<int, 8>());
     };
-    if (ct <= 1) return blocks(std::integral_constant<int, 1>());
-    if (ct <= 2) return blocks(std::integral_constant<int, 2>());
-    if (ct <= 4) return blocks(std::integral_constant<int, 4>());
-    return false;
+    blocks(std::integral_constant<int, 1>());
+    blocks(std::integral_constant<int, 2>());
+    blocks(std::integral_constant<int, 4>());
+    return few.ct > 0;
 }
 
 }  // namespace

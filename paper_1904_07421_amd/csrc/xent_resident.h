@@ -14,6 +14,7 @@
 #pragma once
 
 #include "level_common.h"
+#include "xent_sizes.h"
 
 #include <utility>
 
@@ -21,13 +22,7 @@ namespace jitdb {
 namespace {
 
 constexpr int kResT = 256;
-constexpr int kResRows = 256;            // resident rows of a block
-constexpr int kResTile = 32;             // rows of the other operand in a tile
 constexpr int kResBufs = 3;
-// A block's range is no shorter; where it makes further rounds of blocks, 8.  (Statistics and g with 8 everywhere and with 2: fp32 2304 x 150
-// x 2003 30 + 43 us, 20 + 25; bf16 2000 x 512 x 2000 21 + 28, 16 + 16; with 2 everywhere fp32 4608 x 150 x 10007 79 + 113, 82 + 136.)
-constexpr int kResMinTiles = 2, kResRoundTiles = 8;
-constexpr int kResBlocks = 1024;         // ranges make no more blocks than this
 constexpr int kResInAcc = 44;            // resident fragments that are kept in accumulation registers, of 64 at most
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f, kLn2Low = (float)(0.69314718055994530942 - (double)kLn2);
 
@@ -45,24 +40,6 @@ struct ResArgs {
     char *g; int64_t g_slab, g_part;     // g of the chunk, K-blocked with K = row: slab of 32 rows, class, 64 bytes
     float *db_part;                      // [ranges, at most kResBlocks / class_blocks or so][256 class_blocks]
 };
-// Ranges for `blocks` blocks of resident rows on a chip that holds `places` at once, `tiles` tiles to walk over: more of them where
-// that leaves fewer places idle in the last round, by more than 1 / 64.
-__host__ __device__ inline int res_ranges(int blocks, int tiles, int places) {
-    if (blocks * 32 < places) {          // few rows: fill the chip
-        const int fill = places / (blocks > 0 ? blocks : 1), most = tiles / kResMinTiles;
-        return fill < most ? fill : most > 1 ? most : 1;
-    }
-    int best = 1, best_rounds = (blocks + places - 1) / places;
-    for (int s = 2; s <= 32 && blocks * s <= kResBlocks && tiles >= s * (blocks * s <= places ? kResMinTiles : kResRoundTiles); ++s) {
-        const int rounds = (blocks * s + places - 1) / places;
-        if (rounds * best * 64 < best_rounds * s * 63) { best = s; best_rounds = rounds; }
-    }
-    return best;
-}
-// one wave a SIMD and two sets of accumulators, or two waves and one set
-constexpr bool res_alone(int fragments, bool g) { return fragments > (g ? 8 : 16); }
-constexpr int res_places(int fragments, bool g) { return res_alone(fragments, g) ? 256 : 512; }
-
 template <typename F, int... I>
 __device__ __forceinline__ void static_for_impl(F &&f, std::integer_sequence<int, I...>) { (f(std::integral_constant<int, I>()), ...); }
 template <int N, typename F>

@@ -14,16 +14,12 @@
 namespace jitdb {
 namespace {
 
-constexpr int kTileB = 256;                           // rows of B in a tile
 constexpr int kT = 256;                               // threads of the small kernels
-template <int WM> constexpr int kTileA = WM * 64;     // rows of A; WM: 64-row waves along A (5: four waves along B with all 160)
-template <> constexpr int kTileA<5> = 160;
 template <int WM> constexpr int kTM = WM == 5 ? 5 : 2;
 template <int WM> constexpr int kTN = WM == 5 ? 2 : 4;
 template <int WM> constexpr int kTileT = WM == 4 ? 512 : 256;           // threads
 template <int WM> constexpr int kTileBufs = WM == 4 ? 4 : 3;
 template <int WM> constexpr int kTileBuf = (kTileA<WM> + kTileB) * 64;
-template <int WM> constexpr int kTilePlaces = WM == 4 ? 256 : 512;      // blocks for each of the two products: half of what the chip holds at once
 template <int WM> constexpr int kTileWaves = WM == 4 ? 1 : 2;           // blocks on a CU
 
 // Operands are K-blocked as in operand_offset, in one to three bf16 parts: part p, slab s (32 elements of K), row r
@@ -235,30 +231,11 @@ struct GradArgs {
     void *out;
     float *acc;                     // dV over several chunks of rows
 };
-constexpr uint32_t kLongRange = 1200;      // stages
-constexpr uint32_t kMinStages = 8;       // a range is no shorter
-struct GradPlan {
-    uint32_t b_tiles, nk, stages;   // stages of a part product, of a tile
-    uint32_t total, per, ranges;    // (a stage stands for 8192 elements of g, six times at most: of a chunk of rows far below 2^32)
-};
-__host__ __device__ inline int grad_ranges(int places, int a_tiles) { return places > a_tiles ? places / a_tiles : 1; }      // at most
 template <bool WEIGHTS, int WM>
 __device__ __forceinline__ GradPlan grad_plan(const GradArgs &a) {
     const int rows = chunk_rows(a.n_rows, a.row0, a.max_rows);
-    GradPlan g;
-    g.b_tiles = WEIGHTS ? (a.C + kTileB - 1) / kTileB : (rows + kTileB - 1) / kTileB;
-    g.nk = WEIGHTS ? (rows + 31) / 32 : (a.C + 31) / 32;
-    g.stages = g.nk * a.p.pairs.n;
-    g.total = g.b_tiles * g.stages;
-    // Ranges: dh's and dV's together are as many blocks as the chip holds.  Long ones of several tiles of A are faster one product after
-    // the other, on all of it (both products with joining, bf16 32768 x 512 x 32000 2.15 ms against 2.25; but 16384 rows 1.17 against
-    // 1.15, 8192 x 512 x 16000 305 us against 286, 65536 x 256 x 32000 2.28 ms against 2.16, fp32 3000 x 256 x 8000 194 us against 163).
-    const uint32_t half = grad_ranges(kTilePlaces<WM> / 2, a.a_tiles);
-    const uint32_t most = a.a_tiles > 1 && g.total / half > kLongRange ? grad_ranges(kTilePlaces<WM>, a.a_tiles) : half;
-    const uint32_t per = (g.total + most - 1) / most;
-    g.per = per > kMinStages ? per : kMinStages;
-    g.ranges = (g.total + g.per - 1) / g.per;
-    return g;
+    return make_plan(WEIGHTS ? (a.C + kTileB - 1) / kTileB : (rows + kTileB - 1) / kTileB, WEIGHTS ? (rows + 31) / 32 : (a.C + 31) / 32,
+                     a.p.pairs.n, kTilePlaces<WM>, a.a_tiles);
 }
 template <bool WEIGHTS, int WM>
 __device__ __forceinline__ void grad_product(const GradArgs &a, char *lds, int block) {
@@ -408,10 +385,10 @@ wide_logits_kernel(const LogitArgs a) {
     const int row_tiles = (rows + 255) / 256 * (G == 0 ? 1 : 2), class_tiles = G == 0 ? a.a_tiles : a.b_tiles;
     const int64_t i = xcd_order((int64_t)row_tiles * class_tiles, (int)blockIdx.x);
     if (i < 0) return;
-    // bands of eight row tiles, class tiles one after another inside a band: the blocks of an XCD share them in its L2
-    const int band = (int)(i / (8 * (int64_t)class_tiles)), rem = (int)(i - (int64_t)band * 8 * class_tiles);
-    const int left = row_tiles - band * 8, width = left < 8 ? left : 8;
-    const int ct = rem / width, rt = band * 8 + rem % width;
+    // bands of row tiles, class tiles one after another inside a band: the blocks of an XCD share them in its L2
+    const int band = (int)(i / (kBand * (int64_t)class_tiles)), rem = (int)(i - (int64_t)band * kBand * class_tiles);
+    const int left = row_tiles - band * kBand, width = left < kBand ? left : kBand;
+    const int ct = rem / width, rt = band * kBand + rem % width;
     floatx16 acc[2][4];
     clear_tile(acc);
     const int n_stages = a.nk * a.p.pairs.n;
