@@ -280,7 +280,10 @@ layernorm_kernel(const NormArgs a) {
                 }
             }
         row_sums<G>(off, sq, red + kWide / 64 * (G > 64));
-        const float more = off * a.inv_h, mean = more == more ? m0 + more : m0, left = sq - off * more;       // (an infinite mean stays one)
+        float more = off * a.inv_h, taken = off * more;
+        // up to 2^-23 of the spread, c is the rounding of the differences as likely as what the mean is off by, and the mean stays
+        if (taken < 0x1p-46f * sq) more = taken = 0.0f;
+        const float mean = more == more ? m0 + more : m0, left = sq - taken;       // (an infinite mean stays one)
         const float rstd = 1.0f / sqrtf((left < 0.0f ? 0.0f : left) * a.inv_h + a.eps);        // (below 0 by rounding alone: equal values)
 #pragma unroll
         for (int j = 0; j < NV; ++j) {

@@ -69,3 +69,16 @@ def test_rows_that_are_not_finite():
     y, mean, _ = J.jitdb_layernorm_forward(x, one, one)
     assert float(mean[0]) == float("inf") and float(mean[1]) == -float("inf") and bool(mean[2].isnan())
     assert bool(y[:3].isnan().any(1).all()) and bool(y[3].isfinite().all())
+
+
+@pytest.mark.parametrize("H", [150, 203, 300, 1000, 2100])
+def test_a_mean_whose_sum_is_exact_is_the_quotient(H):
+    """Multiples of 1 / 128 around zero: their sum has no rounding, and the rounded differences may not add one."""
+    import torch
+    import paper_1904_07421_amd as J
+    k = torch.randint(-127, 128, (5000, H), generator=torch.Generator().manual_seed(H))
+    want = (k.sum(1).double() / 128 / H).float()
+    one = torch.ones(H, device="cuda")
+    for dtype in (torch.float32, torch.bfloat16):
+        _, mean, _ = J.jitdb_layernorm_forward((k.float() / 128).to("cuda", dtype), one, one)
+        assert torch.equal(mean.cpu(), want)
