@@ -31,6 +31,7 @@ constexpr int kWaveMax = 2048;
 constexpr int kMaxWidth = 1 << 14;
 constexpr int kForwardBlocks = 8192;     // of the forward pass (2048 take 10 to 15 % longer on a million rows)
 constexpr int kMaxParts = 1024;          // partial sums of the weight gradients: blocks of the backward pass
+constexpr int kChain = 16, kWideChain = 32;       // rows whose terms are added in a row
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
@@ -303,19 +304,23 @@ layernorm_kernel(const NormArgs a) {
 
 // The rows of a block add to the same columns: every lane keeps the weight gradients of its columns, the groups of a block are
 // added in order through LDS, the blocks by layernorm_reduce_kernel, also in order: the result does not depend on timing.
+// A lane's sums start anew every kChain rows, and those before are added to its second ones: one chain over all its rows (1.18 M x 512:
+// 288) would lose up to half a step of the whole sum in each addition, 5e-6 of it where the terms are alike; norm-wise, of random terms,
+// 3.3e-7 became 1.4e-7.
 template <typename T, typename GT, int G, int NV>
 __global__ void __launch_bounds__(G <= 64 ? kT : kWide)
 layernorm_backward_kernel(const NormArgs a) {
     constexpr int V = kVec<T>, THREADS = G <= 64 ? kT : kWide, GROUPS = THREADS / G;
     __shared__ float red[G <= 64 ? 1 : 2 * kWide / 64];
     constexpr int W = G * NV * V;
-    __shared__ float sums[2 * W];
+    __shared__ float sums[2 * W * GROUPS];          // KEEP: the second sums, in lane order; else the first, in column order
     int l = threadIdx.x % G;
     const int H = a.H;
     const T *x = static_cast<const T *>(a.x);
     const GT *gy = static_cast<const GT *>(a.gy);
     const uint64_t start = a.drop.state ? drop_start(a.drop) : 0;
-    // gamma and the gradients of the longest rows do not fit the registers of 512 threads: the gradients stay in LDS
+    // gamma and the gradients of the longest rows do not fit the registers of 512 threads: the gradients stay in LDS, their second sums
+    // where the block's go
     constexpr bool KEEP = G <= 64;
     constexpr bool AHEAD = G <= 64 && NV * V <= 16;      // the next row is on its way while this one is worked on, where registers allow
     float gamma[KEEP ? NV : 1][V], dgamma[KEEP ? NV : 1][V], dbeta[KEEP ? NV : 1][V];
@@ -346,6 +351,29 @@ layernorm_backward_kernel(const NormArgs a) {
             next_g[j] = load_row<GT, V>(gy + r * H + c, H - c);
         }
     };
+    float *part = a.part + (int64_t)blockIdx.x * 2 * H;
+    bool begun = false;
+    auto second = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+            for (int k = 0; k < V; ++k) {
+                if constexpr (KEEP) {
+                    float &sg = sums[(j * V + k) * THREADS + threadIdx.x], &sb = sums[((NV + j) * V + k) * THREADS + threadIdx.x];
+                    sg = begun ? sg + dgamma[j][k] : dgamma[j][k];
+                    sb = begun ? sb + dbeta[j][k] : dbeta[j][k];
+                    dgamma[j][k] = dbeta[j][k] = 0.0f;
+                } else {
+                    const int c = (j * G + l) * V + k;
+                    if (c >= H) continue;
+                    part[c] = begun ? part[c] + sums[c] : sums[c];
+                    part[H + c] = begun ? part[H + c] + sums[W + c] : sums[W + c];
+                    sums[c] = sums[W + c] = 0.0f;
+                }
+            }
+        begun = true;
+    };
+    int chain = 0;
     if (AHEAD && row < a.n) fetch(row);
     for (; row < a.n; row += step) {
         if constexpr (!AHEAD) fetch(row);
@@ -390,35 +418,30 @@ layernorm_backward_kernel(const NormArgs a) {
             for (int k = 0; k < V; ++k) g[j][k] = (g[j][k] - s1 - xh[j][k] * s2) * rstd;
             store_row_piece<float, V>(a.dx + row * H + c, H - c, g[j]);
         }
-    }
-    float *part = a.part + (int64_t)blockIdx.x * 2 * H;
-    if constexpr (KEEP)
-        for (int q = 0; q < GROUPS; ++q) {
-            if ((int)threadIdx.x / G == q)
-#pragma unroll
-                for (int j = 0; j < NV; ++j)
-#pragma unroll
-                    for (int k = 0; k < V; ++k) {
-                        const int c = (j * G + l) * V + k;
-                        sums[c] = q ? sums[c] + dgamma[j][k] : dgamma[j][k];
-                        sums[W + c] = q ? sums[W + c] + dbeta[j][k] : dbeta[j][k];
-                    }
-            __syncthreads();
+        if (++chain == (KEEP ? kChain : kWideChain)) {
+            second();
+            chain = 0;
         }
-    else
+    }
+    second();
+    if constexpr (KEEP) {
         __syncthreads();
-    for (int c = threadIdx.x; c < H; c += THREADS) {
-        part[c] = sums[c];
-        part[H + c] = sums[W + c];
+        for (int c = threadIdx.x; c < 2 * H; c += THREADS) {
+            const int of = c < H ? c : c - H, piece = of / V, at = ((c < H ? 0 : NV) + piece / G) * V + of % V;
+            float s = 0.0f;
+#pragma unroll
+            for (int q = 0; q < GROUPS; ++q) s += sums[at * THREADS + q * G + piece % G];
+            part[c] = s;
+        }
     }
 }
 
-// column c of [n_parts, 2H], 16 parts at a time and the sixteen sums in order
+// column c of [n_parts, 2H], 16 parts at a time and the sixteen sums in order; in fp64, which costs nothing here
 __global__ void __launch_bounds__(1024)
 layernorm_reduce_kernel(const float *__restrict__ part, int n_parts, int H, float *__restrict__ dgamma, float *__restrict__ dbeta) {
-    __shared__ float sums[16][64];
+    __shared__ double sums[16][64];
     const int l = threadIdx.x & 63, q = threadIdx.x >> 6, c = blockIdx.x * 64 + l;
-    float s = 0.0f;
+    double s = 0.0;
     if (c < 2 * H)
 #pragma unroll 8
         for (int p = q; p < n_parts; p += 16) s += part[(int64_t)p * 2 * H + c];
@@ -426,8 +449,8 @@ layernorm_reduce_kernel(const float *__restrict__ part, int n_parts, int H, floa
     __syncthreads();
     if (q || c >= 2 * H) return;
     for (int k = 1; k < 16; ++k) s += sums[k][l];
-    if (c < H) dgamma[c] = s;
-    else dbeta[c - H] = s;
+    if (c < H) dgamma[c] = (float)s;
+    else dbeta[c - H] = (float)s;
 }
 
 int norm_groups(int H, int vec) {       // rows that a block works on at once

@@ -82,3 +82,25 @@ def test_a_mean_whose_sum_is_exact_is_the_quotient(H):
     for dtype in (torch.float32, torch.bfloat16):
         _, mean, _ = J.jitdb_layernorm_forward((k.float() / 128).to("cuda", dtype), one, one)
         assert torch.equal(mean.cpu(), want)
+
+
+@pytest.mark.parametrize("n,H,lanes,chain", [(1000000, 512, 4096, 16), (4000000, 24, 16384, 16), (300000, 1030, 4096, 16), (200000, 2049, 1024, 32)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_weight_gradients_of_many_rows_alike(n, H, lanes, chain, dtype):
+    """Terms that are all alike are rounded alike: each addition loses up to half a step of the sum so far, k of them (k + 1) / 2 half
+    steps of the last.  A lane adds `chain` terms, then what it has of those before; at most 16 lanes are added in a block, the blocks in fp64."""
+    import torch
+    import paper_1904_07421_amd as J
+    print(f"weight gradients n={n} H={H} {dtype}", flush=True)
+    ones = torch.ones((n, H), dtype=torch.float32 if dtype == "f32" else torch.bfloat16, device="cuda")
+    mean, rstd, gamma = torch.zeros(n, device="cuda"), torch.ones(n, device="cuda"), torch.ones(H, device="cuda")
+    second = -(-(-(-n // lanes)) // chain)
+    bound = ((chain + 1) / 2 + (second + 1) / 2 + (16 + 1) / 2 + 1) * U32
+    for v in (0.9869921803474426, 0.5594824552536011, 0.7893792390823364):
+        gy = torch.full((n, H), v, device="cuda")
+        _, dgamma, dbeta = J.jitdb_layernorm_backward(ones, gamma, mean, rstd, gy)
+        want = n * float(gy[0, 0])
+        for name, got in (("dgamma", dgamma), ("dbeta", dbeta)):
+            off = float((got.double() / want - 1).abs().max())
+            assert off <= bound, (name, v, off, bound)
+        del gy
