@@ -88,3 +88,62 @@ def test_fp32_values_above_the_largest_bf16(H, C):
     loss_err, lse_err, dh_err, dV_err, db_err, out = _tolerances(h, V, None, label, gloss, "f32", "f32", loss, lse, g, p)
     for t, want, err in ((loss_t, loss, loss_err), (lse_t, lse, lse_err), (db_t, db, db_err), (dV_t, dV, dV_err), (dh_t, dh, dh_err)):
         assert np.all(np.abs(_host(t) - want) <= err * (1 + out) + out * np.abs(want) + 1e-36)
+
+
+@pytest.mark.parametrize("C", [7, 300])
+def test_more_than_2_to_32_elements(C):
+    """Offsets past 32 bits in states, their layouts and gradients: the last rows of a batch are what they are alone."""
+    import torch
+    import paper_1904_07421_amd as J
+    H = 512
+    n = (1 << 32) // H + 5
+    print(f"xent 2^32 elements C={C}", flush=True)
+    torch.manual_seed(C)
+    h = torch.zeros((n, H), dtype=torch.bfloat16, device="cuda")
+    h[-7:] = torch.randn(7, H, device="cuda").bfloat16()
+    V, b = (torch.randn(C, H, device="cuda") / 16).bfloat16(), torch.randn(C, device="cuda")
+    label = torch.full((n,), 3, dtype=torch.int32, device="cuda")
+    label[-7:] = torch.randint(0, C, (7,), device="cuda", dtype=torch.int32)
+    gloss = torch.zeros(n, device="cuda")
+    gloss[-7:] = torch.rand(7, device="cuda") + 0.5
+    loss, lse = J.jitdb_softmax_xent_forward(h, V, label, b=b)
+    dh, dV, db = J.jitdb_softmax_xent_backward(h, V, label, lse, gloss=gloss, b=b)
+    tail = [t[-7:].contiguous() for t in (h, label, gloss)]
+    loss7, lse7 = J.jitdb_softmax_xent_forward(tail[0], V, tail[1], b=b)
+    dh7, dV7, db7 = J.jitdb_softmax_xent_backward(tail[0], V, tail[1], lse7, gloss=tail[2], b=b)
+    assert bool((lse[:-7] == lse[0]).all()) and bool((loss[:-7] == loss[0]).all())
+    want = float(torch.logsumexp(b.double(), 0))
+    # of C exponentials and their logarithm, as in the tests of sizes; the rows alone are cut into other ranges, sums in another order
+    close = (C + 8) * 2.0 ** -24 + 2.0 ** -20
+    assert abs(float(lse[0]) - want) <= close + 4 * 2.0 ** -24 * abs(want)
+    assert float((lse[-7:] - lse7).abs().max()) <= 2 * close + 8 * 2.0 ** -24 * float(lse7.abs().max())
+    assert float((loss[-7:] - loss7).abs().max()) <= 2 * close + 8 * 2.0 ** -24 * float(lse7.abs().max() + loss7.abs().max())
+    assert not bool(dh[:-7].any())
+    for got, ref in ((dh[-7:], dh7), (dV, dV7), (db, db7)):
+        # seven rows' terms, each good to 2^-18 (exponentials and what they are taken of), as a norm
+        assert float((got - ref).norm() / ref.norm()) <= 2.0 ** -17
+
+
+@pytest.mark.parametrize("dtype,H,C,grad", [(*s, g) for s in SHAPES for g in ("f32", "bf16") if s[0] == "bf16" or g == "f32"])
+def test_a_mask_of_the_lowest_value_is_a_mask(dtype, H, C, grad):
+    """Classes behind the type's lowest value, at the front, at the end and in between: what -inf gives, bit for bit."""
+    import torch
+    import paper_1904_07421_amd as J
+    dt, gdt = (torch.float32 if k == "f32" else torch.bfloat16 for k in (dtype, grad))
+    torch.manual_seed(C + H)
+    n = 130
+    h, V = torch.rand(n, H, device="cuda").to(dt), (torch.randn(C, H, device="cuda") / H ** 0.5).to(dt)
+    out = torch.rand(C, device="cuda") < 0.3
+    out[: C // 3] = out[-C // 5:] = True
+    out[C // 2] = False
+    classes = (~out).nonzero().flatten()
+    label = classes[torch.randint(0, len(classes), (n,), device="cuda")].int()
+    got = []
+    for low in (-float("inf"), torch.finfo(torch.float32).min, -1e30):
+        b = torch.randn(C, generator=torch.Generator().manual_seed(1)).cuda()
+        b[out] = low
+        loss, lse = J.jitdb_softmax_xent_forward(h, V, label, b=b)
+        got.append((loss, lse) + J.jitdb_softmax_xent_backward(h, V, label, lse, b=b, grad_dtype=gdt))
+        assert all(bool(t.isfinite().all()) for t in got[-1])
+    for other in got[1:]:
+        assert all(torch.equal(u, v) for u, v in zip(got[0], other))
