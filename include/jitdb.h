@@ -482,7 +482,10 @@ int jitdb_layernorm_backward(const void *x, const float *gamma, const float *mea
                              void *workspace, size_t workspace_bytes, void *hip_stream);
 
 /*
- * Softmax cross entropy over classes or words, with its gradient.  The logits of the batch are never kept.
+ * Softmax cross entropy over classes or words, with its gradient.  The forward pass keeps no logits.  The backward pass keeps their
+ * derivatives, in the workspace and in pieces of the batch: of up to 4 GiB (2 bytes a logit, 6 where gradients leave in fp32) or of
+ * 256 rows, whichever is more.  Workspaces go by n_rows, whether rows have a label or not.  (Up to 64 classes, where the kernels for
+ * few classes take the width, there is no such workspace.)
  *     z_nc = <h_n, V_c> + b_c      lse_n = log sum_c exp(z_nc)      loss_n = lse_n - z_n,label(n)
  *
  *   h        dev [n_rows, H] in dtype elements
@@ -500,7 +503,8 @@ int jitdb_layernorm_backward(const void *x, const float *gamma, const float *mea
  * 1 for every row), and returns, all overwritten,
  *     dh [n_rows, H], dV [n_classes, H] in grad_dtype elements, db [n_classes] in fp32.
  * grad_dtype is JITDB_F32 (dh is then the gh of jitdb_treelstm_backward, if h is the forward's), or JITDB_BF16 for bf16
- * operands: the derivatives of the logits are then bf16 operands of the two products, which takes about 0.4 of the time.
+ * operands: the derivatives of the logits are then bf16 operands of the two products, which takes about 0.4 of the time and leaves
+ * 1.4 times the error (norm-wise) of rounding exact gradients to bf16.
  * n_rows == 0 zeroes dV and db.
  */
 #define JITDB_MAX_CLASSES (1 << 22)

@@ -15,8 +15,8 @@
 //     mix64(mix64(seed) + (first + i / 2) golden)                  (SplitMix64 with a mixed key; seed, first: state[0], state[1])
 // is at least p 2^32.  The mask is a function of i: the backward pass computes it again and nothing is stored.
 //
-// All kernels are bound by memory (a large copy reaches 4.7 TB/s).  1.18 M rows of 512, bf16: forward 523 us, with dropout 573 (4.2 TB/s),
-// backward 1064 (4.5 TB/s; fp32 dx out); dropout of 1.18 M x 300 bf16 262 us (5.4 TB/s).
+// All kernels are bound by memory (copies reach 4.5 to 5.4 TB/s, by their shape).  1.18 M rows of 512, bf16: forward 510 us (4.7 TB/s), with
+// dropout 591, backward 1068 (4.5 TB/s; fp32 dx out); dropout of 1.18 M x 300 bf16 258 us (5.5 TB/s).
 
 #include "common.h"
 
@@ -26,8 +26,8 @@ namespace jitdb {
 namespace {
 
 constexpr int kT = 256;
-constexpr int kWide = 512;               // threads that share a row of more than kWaveMax values
-constexpr int kWaveMax = 2048;
+constexpr int kWide = 512;               // threads that share a row of more than kWaveMax values: the variant of kMaxWidth, whatever its length
+constexpr int kWaveMax = 2048;           // (fp32 forward and backward: 120000 x 2048 350 and 568 us, 100000 x 2049 1226 and 2491, 16000 x 16384 490 and 708)
 constexpr int kMaxWidth = 1 << 14;
 constexpr int kForwardBlocks = 8192;     // of the forward pass (2048 take 10 to 15 % longer on a million rows)
 constexpr int kMaxParts = 1024;          // partial sums of the weight gradients: blocks of the backward pass

@@ -23,8 +23,8 @@ constexpr bool few_variant(int element, int ct, int nb) {
     return ct * nb * (16 / element) <= 32 && few_table_bytes(ct, nb) + 2 * kFewRows * (ct * 64 + 4) <= 160 * 1024;
 }
 struct FewSizes { int ct, nb; };         // 0: no variant
-// Taken wherever one fits (forward and backward of 100 k rows, the last size that fits and the next: fp32 150 x 64 218 us, 150 x 65 720;
-// 512 x 32 323, 512 x 48 1247; bf16 512 x 64 444, 512 x 65 606).
+// Taken wherever one fits (forward and backward of 100 k rows with fp32 gradients, the last size that fits and the next: fp32 150 x 64
+// 215 us, 150 x 65 609; 512 x 32 327, 512 x 48 1234; bf16 512 x 64 445, 512 x 65 741).
 constexpr FewSizes few_sizes(int element, int H, int C) {
     const int blocks = (int)ceil_div(H, 64 * (16 / element));
     const int ct = C <= 16 ? 1 : C <= 32 ? 2 : C <= 64 ? 4 : 0, nb = blocks <= 1 ? 1 : blocks <= 2 ? 2 : blocks <= 4 ? 4 : blocks <= 8 ? 8 : 0;
@@ -90,7 +90,7 @@ constexpr int kMaxClasses = 1 << 22;
 constexpr int kMaxWidth = 1 << 14;
 constexpr int kLabelBlock = 1024, kLabelBlocks = 2048;     // labels of a block of the listing kernels at least, most blocks of them
 constexpr int64_t kStatBytes = 512ll << 20;   // of tile statistics of wide states kept at once (forward) ...
-constexpr int64_t kGradBytes = 4ll << 30;     // ... and of g (backward): rows beyond come in further chunks
+constexpr int64_t kGradBytes = 4ll << 30;     // ... and of g (backward): rows beyond come in further chunks, of 256 rows at least
 struct Sizes {
     int64_t n, n_pad;          // rows at most, and rounded up to whole tiles
     int H, C, Hk, Hf, Cp;      // widths: of K (states), of the turned states' rows, classes in whole tiles
