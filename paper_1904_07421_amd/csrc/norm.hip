@@ -31,6 +31,7 @@ constexpr int kWaveMax = 2048;           // (fp32 forward and backward: 120000 x
 constexpr int kMaxWidth = 1 << 14;
 constexpr int kForwardBlocks = 8192;     // of the forward pass (2048 take 10 to 15 % longer on a million rows)
 constexpr int kMaxParts = 1024;          // partial sums of the weight gradients: blocks of the backward pass
+constexpr float kFar = 16.0f;            // |mean| / spread up to which the rounding of a mean (2^-20 of the spread) stays in the backward pass
 constexpr int kChain = 16, kWideChain = 32;       // rows whose terms are added in a row
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
@@ -311,7 +312,7 @@ template <typename T, typename GT, int G, int NV>
 __global__ void __launch_bounds__(G <= 64 ? kT : kWide)
 layernorm_backward_kernel(const NormArgs a) {
     constexpr int V = kVec<T>, THREADS = G <= 64 ? kT : kWide, GROUPS = THREADS / G;
-    __shared__ float red[G <= 64 ? 1 : 2 * kWide / 64];
+    __shared__ float red[G <= 64 ? 1 : 3 * kWide / 64];
     constexpr int W = G * NV * V;
     __shared__ float sums[2 * W * GROUPS];          // KEEP: the second sums, in lane order; else the first, in column order
     int l = threadIdx.x % G;
@@ -386,6 +387,18 @@ layernorm_backward_kernel(const NormArgs a) {
             unpack<GT, V>(next_g[j], g[j]);
         }
         if (AHEAD && row + step < a.n) fetch(row + step);
+        // A mean is kept to 2^-24 of itself: where that is much of a row's spread, what is left of it comes off the centred values here too
+        float more = 0.0f;
+        const bool far = fabsf(mean) * rstd > kFar;
+        if (__any(far)) {
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+#pragma unroll
+                for (int k = 0; k < V; ++k)
+                    if ((j * G + l) * V + k < H) more += xh[j][k] - mean;
+            more = row_sum<G>(more, red + 2 * kWide / 64 * (G > 64)) * a.inv_h;
+            more = far ? more : 0.0f;                          // (a row's result does not depend on those beside it in a wave)
+        }
         float s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
@@ -393,7 +406,7 @@ layernorm_backward_kernel(const NormArgs a) {
             if (a.drop.state) apply_drop<V>(a.drop, start, (uint64_t)row * H + c, g[j]);
 #pragma unroll
             for (int k = 0; k < V; ++k) {
-                xh[j][k] = (xh[j][k] - mean) * rstd;
+                xh[j][k] = (xh[j][k] - mean - more) * rstd;
                 if (c + k >= H) xh[j][k] = g[j][k] = 0.0f;
                 if constexpr (KEEP) {
                     dgamma[j][k] += g[j][k] * xh[j][k];

@@ -104,3 +104,53 @@ def test_weight_gradients_of_many_rows_alike(n, H, lanes, chain, dtype):
             off = float((got.double() / want - 1).abs().max())
             assert off <= bound, (name, v, off, bound)
         del gy
+
+
+@pytest.mark.parametrize("H", WIDTHS)
+@pytest.mark.parametrize("far", [1e2, 1e4, -1e5])
+def test_gradients_of_rows_far_from_zero(H, far):
+    """dx and dgamma take the centred values: the mean that the forward pass returns is rounded, by 3e-3 of the spread at 1e5."""
+    import torch
+    import paper_1904_07421_amd as J
+    n = 40
+    rng = np.random.default_rng([H, int(abs(far)), 1])
+    x = (far + rng.standard_normal((n, H))).astype(np.float32)
+    gy, gamma = rng.standard_normal((n, H)).astype(np.float32), rng.standard_normal(H).astype(np.float32)
+    x_t, gy_t, gamma_t = (torch.from_numpy(a).cuda() for a in (x, gy, gamma))
+    _, mean_t, rstd_t = J.jitdb_layernorm_forward(x_t, gamma_t, gamma_t)
+    got = [t.cpu().numpy().astype(np.float64) for t in J.jitdb_layernorm_backward(x_t, gamma_t, mean_t, rstd_t, gy_t)]
+    x, gy, gamma = (a.astype(np.float64) for a in (x, gy, gamma))
+    dx, dgamma, dbeta = O.layernorm_backward(x, gamma, gy, 1e-5)
+    _, mean, rstd = O.layernorm(x, gamma, 0.0, 1e-5)
+    rstd = rstd[:, None]
+    k = _depth(H) + 2
+    first = k * U32 * np.abs(x).mean(1, keepdims=True)              # of the first mean, forward; the second is closer than that
+    d = np.abs(x - mean[:, None]) + first
+    corr = k * U32 * d.mean(1, keepdims=True)
+    rstd_rel = 0.5 * (2 * k * U32 * (d ** 2).mean(1, keepdims=True) + 2 * first * corr) * rstd ** 2 * (1 + 1e-3) + 4 * U32
+    xhat = (x - mean[:, None]) * rstd
+    xhat_err = rstd * (corr + 3 * U32 * d) + (rstd_rel + 2 * U32) * d * rstd
+    a = np.abs(gy * gamma)
+    mean_a, mean_xa = a.mean(1, keepdims=True), (a * np.abs(xhat)).mean(1, keepdims=True)
+    dx_err = rstd * (k * U32 * mean_a + np.abs(xhat) * (k * U32 * mean_xa + (a * xhat_err).mean(1, keepdims=True)) + xhat_err * mean_xa
+                     + 6 * U32 * (a + mean_a + np.abs(xhat) * mean_xa)) + rstd_rel * np.abs(dx)
+    assert np.all(np.abs(got[0] - dx) <= dx_err)
+    assert np.all(np.abs(got[1] - dgamma) <= (n + 4) * U32 * np.abs(gy * xhat).sum(0) + (np.abs(gy) * xhat_err).sum(0))
+    assert np.all(np.abs(got[2] - dbeta) <= (n + 4) * U32 * np.abs(gy).sum(0))
+
+
+@pytest.mark.parametrize("H", [20, 60, 100, 300, 2100])
+def test_a_row_does_not_depend_on_its_neighbours(H):
+    import torch
+    import paper_1904_07421_amd as J
+    torch.manual_seed(H)
+    x, gy, gamma = torch.randn(64, H, device="cuda"), torch.randn(64, H, device="cuda"), torch.randn(H, device="cuda")
+    near = torch.arange(64, device="cuda") % 3 != 1
+    x[~near] += 3e4
+    y, mean, rstd = J.jitdb_layernorm_forward(x, gamma, gamma)
+    dx = J.jitdb_layernorm_backward(x, gamma, mean, rstd, gy)[0]
+    x0 = x[near].contiguous()
+    y0, mean0, rstd0 = J.jitdb_layernorm_forward(x0, gamma, gamma)
+    dx0 = J.jitdb_layernorm_backward(x0, gamma, mean0, rstd0, gy[near].contiguous())[0]
+    for a, b in ((y, y0), (mean, mean0), (rstd, rstd0), (dx, dx0)):
+        assert torch.equal(a[near], b)
