@@ -504,7 +504,8 @@ int jitdb_layernorm_backward(const void *x, const float *gamma, const float *mea
  *     dh [n_rows, H], dV [n_classes, H] in grad_dtype elements, db [n_classes] in fp32.
  * grad_dtype is JITDB_F32 (dh is then the gh of jitdb_treelstm_backward, if h is the forward's), or JITDB_BF16 for bf16
  * operands: the derivatives of the logits are then bf16 operands of the two products, which takes about 0.4 of the time and leaves
- * 1.4 times the error (norm-wise) of rounding exact gradients to bf16.
+ * up to 1.4 times the error (norm-wise) of rounding exact gradients to bf16, and no more than that error where every gloss is the
+ * same and labels are improbable: only the significand of gloss beside the largest one's is rounded.
  * n_rows == 0 zeroes dV and db.
  */
 #define JITDB_MAX_CLASSES (1 << 22)

@@ -14,8 +14,11 @@
 // (8 mantissa bits each, 24 in all) and a product of two of them is the six part products of weight 2^-16 and more; what is left out
 // is about 2^-23 of the product at most, two roundings of an fp32 multiplication, at 2.5 times the rate of the fp32 matrix instructions.
 // g, computed in fp32, is multiplied as one bf16 part where the gradients leave in bf16 (a rounding of 2^-8 on terms of a sum that
-// is itself rounded to 2^-8: norm-wise 2.4e-3 of the gradients, of which rounding them alone is 1.7e-3), in three parts where they leave
+// is itself rounded to 2^-8: norm-wise up to 2.4e-3 of the gradients, of which rounding them alone is 1.7e-3), in three parts where they leave
 // in fp32 (two would leave 2.5e-6 of them, as a norm: more than the fp32 sums do).  The bias' gradient sums fp32 values.
+// Of a likely label's competitors g is small, its own is nearly -gloss: where that is rounded, all of the row's gradient is off by as much,
+// and where every gloss is the same (a mean), all gradients in the same direction.  So the one part is of g / m, m the significand of the
+// largest |gloss|: weights that are alike are powers of two then, and m is multiplied into the sums, in fp32.
 
 #include "xent_few.h"
 #include "xent_tile.h"
@@ -37,31 +40,77 @@ struct RowList {
     int32_t *row_of;            // [N + pad]
     int32_t *label_of;          // forward: the same rows' labels (-1: names no class)
     float *side;                // backward: records of 32 rows, as in ResArgs
+    float *big, *scale;         // gradients in bf16: largest |gloss| of each block of labels; its significand over all of them
     float *loss_out, *lse_out;  // forward: 0 for rows without a label
 };
+// what a row adds to the largest |gloss|
+__device__ __forceinline__ float weight_size(float w, int32_t label) { return label != -1 && fabsf(w) < INFINITY ? fabsf(w) : 0.0f; }
+// in [1, 2); 1 where there is none (0, and what is below the normal range)
+__device__ __forceinline__ float significand(float v) {
+    const uint32_t u = __float_as_uint(v);
+    return u >> 23 ? __uint_as_float((u & 0x7FFFFFu) | 0x3F800000u) : 1.0f;
+}
+// sum and maximum over a block
+__device__ __forceinline__ void block_sum_max(int &c, float &big, int32_t (&red)[kT / 64], float (&red_big)[kT / 64]) {
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) {
+        c += __shfl_xor(c, m);
+        big = fmaxf(big, __shfl_xor(big, m));
+    }
+    if ((threadIdx.x & 63) == 0) {
+        red[threadIdx.x >> 6] = c;
+        red_big[threadIdx.x >> 6] = big;
+    }
+    __syncthreads();
+    c = red[0] + red[1] + red[2] + red[3];
+    big = fmaxf(fmaxf(red_big[0], red_big[1]), fmaxf(red_big[2], red_big[3]));
+}
 __device__ __forceinline__ void count_labels(const RowList &a, int block) {
     __shared__ int32_t red[kT / 64];
+    __shared__ float red_big[kT / 64];
     int c = 0;
+    float big = 0.0f;
+    const bool weights = a.scale && a.gloss;
     const int64_t at = (int64_t)block * a.per_block;
-    for (int i = threadIdx.x; i < a.per_block; i += kT) c += at + i < a.n && a.label[at + i] != -1;
+    for (int i0 = 0; i0 < a.per_block; i0 += kLabelBlock) {     // (all loads of a turn on their way at once)
+        constexpr int TURN = kLabelBlock / kT;
+        int32_t label[TURN];
+        float w[TURN];
 #pragma unroll
-    for (int m = 1; m < 64; m <<= 1) c += __shfl_xor(c, m);
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = c;
-    __syncthreads();
-    if (threadIdx.x == 0) a.counts[block] = red[0] + red[1] + red[2] + red[3];
+        for (int u = 0; u < TURN; ++u) {
+            const int64_t i = at + i0 + u * kT + threadIdx.x;
+            label[u] = i < a.n ? a.label[i] : -1;
+            w[u] = weights && i < a.n ? a.gloss[i] : 0.0f;
+        }
+#pragma unroll
+        for (int u = 0; u < TURN; ++u) {
+            c += label[u] != -1;
+            big = fmaxf(big, weight_size(w[u], label[u]));
+        }
+    }
+    block_sum_max(c, big, red, red_big);
+    if (threadIdx.x == 0) {
+        a.counts[block] = c;
+        if (weights) a.big[block] = big;
+    }
 }
 // Lists the rows in ascending order.  The last block also knows their number, and fills the last 256 rows' records.
 __global__ void __launch_bounds__(kT)
 label_rows_kernel(const RowList a) {
     __shared__ int32_t red[kT / 64];
+    __shared__ float red_big[kT / 64];
     const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
-    int before = 0;
-    for (int i = t; i < (int)blockIdx.x; i += kT) before += a.counts[i];
-#pragma unroll
-    for (int m = 1; m < 64; m <<= 1) before += __shfl_xor(before, m);
-    if (lane == 0) red[wave] = before;
-    __syncthreads();
-    int base = red[0] + red[1] + red[2] + red[3];
+    const bool weights = a.scale && a.gloss;
+    int base = 0;
+    float big = 0.0f;
+    for (int i = t; i < (int)gridDim.x && gridDim.x > 1; i += kT) {
+        base += i < (int)blockIdx.x ? a.counts[i] : 0;
+        if (weights) big = fmaxf(big, a.big[i]);
+    }
+    if (weights && gridDim.x == 1)                              // (a single block is not asked before)
+        for (int i = t; i < a.n; i += kT) big = fmaxf(big, weight_size(a.gloss[i], a.label[i]));
+    block_sum_max(base, big, red, red_big);
+    const float scale = significand(big);
     auto record = [&](int at, float lse, float w, int32_t label) {
         float *rec = a.side + (int64_t)(at >> 5) * 128 + (at & 31);
         rec[0] = lse;
@@ -81,7 +130,7 @@ label_rows_kernel(const RowList a) {
         if (has) {
             const bool known = label >= 0 && label < a.C;           // a label that names no class makes its row NaN
             a.row_of[at] = (int32_t)i;
-            if (a.side) record(at, a.lse[i] * a.lse_scale, !known ? __builtin_nanf("") : a.gloss ? a.gloss[i] : 1.0f, known ? label : -1);
+            if (a.side) record(at, a.lse[i] * a.lse_scale, !known ? __builtin_nanf("") : a.gloss ? a.gloss[i] / scale : 1.0f, known ? label : -1);
             else a.label_of[at] = known ? label : -1;
         } else if (i < a.n && a.loss_out) {
             a.loss_out[i] = 0.0f;
@@ -90,7 +139,10 @@ label_rows_kernel(const RowList a) {
         base += red[0] + red[1] + red[2] + red[3];
     }
     if (blockIdx.x != gridDim.x - 1) return;
-    if (t == 0) *a.n_rows = base;
+    if (t == 0) {
+        *a.n_rows = base;
+        if (a.scale) *a.scale = scale;
+    }
     if (a.side && base + t < (base + 255) / 256 * 256) record(base + t, INFINITY, 0.0f, -1);       // exp(z - inf) = 0
 }
 
@@ -287,7 +339,7 @@ clear_kernel(O *__restrict__ p, int64_t n) {
 // ---- workspaces ----------------------------------------------------------------------------------------
 struct Space {
     int32_t *counts, *n_rows, *row_of, *label_of;
-    float *side, *label_z, *bias, *db_part, *part_h, *part_v, *acc_v;
+    float *big, *scale, *side, *label_z, *bias, *db_part, *part_h, *part_v, *acc_v;
     float2 *stat;
     Operand h, v, ht, g;
     size_t bytes;
@@ -314,6 +366,10 @@ Space carve(const Sizes &s, bool backward, void *base) {
         w.stat = c.take<float2>(s.res ? (size_t)res_most(s.n_pad / kResRows, s.class_tiles) * kResRows : (size_t)(s.Cp / 64) * s.stat_rows);
     } else {
         w.side = c.take<float>((size_t)s.n_pad * 4);
+        if (s.g_parts == 1) {
+            w.big = c.take<float>(s.label_blocks);
+            w.scale = c.take<float>(1);
+        }
         w.ht = take_operand(c, s.parts, s.n_pad / 32, s.Hf);
         w.g = take_operand(c, s.g_parts, s.grad_rows / 32, s.Cp);
         w.db_part = c.take<float>(s.res ? (size_t)res_most(s.Cp / kResRows, s.grad_rows / kResTile) * kResRows : (size_t)(s.grad_rows / 64) * s.Cp);
@@ -438,7 +494,7 @@ int run_backward_xent(const T *h, const T *V, const float *b, const RowList &lis
     gh.part = w.part_h; gh.out = dh; gh.row_of = w.row_of;
     gv.p.A = w.ht; gv.p.B = w.g; gv.p.pairs = make_pairs(s.parts, s.g_parts);
     gv.part = w.part_v; gv.out = dV; gv.acc = w.acc_v;
-    for (GradArgs *g : {&gh, &gv}) { g->a_tiles = s.a_tiles; g->n_rows = w.n_rows; g->max_rows = s.grad_rows; g->H = s.H; g->C = s.C; }
+    for (GradArgs *g : {&gh, &gv}) { g->scale = w.scale; g->a_tiles = s.a_tiles; g->n_rows = w.n_rows; g->max_rows = s.grad_rows; g->H = s.H; g->C = s.C; }
     for (int64_t r0 = 0; r0 < s.n; r0 += s.grad_rows) {
         const int64_t rows = s.n - r0 < s.grad_rows ? s.n - r0 : s.grad_rows, row_tiles = ceil_div(rows, 256);
         ra.row0 = a.row0 = gh.row0 = gv.row0 = (int)r0;
@@ -453,7 +509,7 @@ int run_backward_xent(const T *h, const T *V, const float *b, const RowList &lis
             JITDB_LAUNCH_CHECK();
         }
         gv.p.A.at = w.ht.at + r0 / 32 * w.ht.slab;
-        const BiasArgs bias = {w.db_part, db, s.Cp, s.res ? res_places(s.parts * s.res, true) : 0};
+        const BiasArgs bias = {w.db_part, db, w.scale, s.Cp, s.res ? res_places(s.parts * s.res, true) : 0};
         rc = s.wm == 4 ? run_grad_products<4, O>(row_tiles, gh, gv, bias, st) : s.wm == 5 ? run_grad_products<5, O>(row_tiles, gh, gv, bias, st)
                                                                                           : run_grad_products<2, O>(row_tiles, gh, gv, bias, st);
         if (rc != JITDB_OK) return rc;
@@ -575,7 +631,7 @@ extern "C" int jitdb_softmax_xent_backward(const void *h, const void *V, const f
     const Space w = carve(s, true, workspace);
     RowList list = {};
     list.label = label; list.lse = lse; list.gloss = gloss; list.n = n_rows; list.C = n_classes; list.counts = w.counts;
-    list.n_rows = w.n_rows; list.row_of = w.row_of; list.side = w.side;
+    list.n_rows = w.n_rows; list.row_of = w.row_of; list.side = w.side; list.big = w.big; list.scale = w.scale;
     list.lse_scale = grad_dtype == JITDB_F32 ? 1.0f : kLog2e;          // as the kernels' exponentials want it
     if (dtype == JITDB_F32)
         return run_backward_xent<float, float>(static_cast<const float *>(h), static_cast<const float *>(V), b, list, s, w,

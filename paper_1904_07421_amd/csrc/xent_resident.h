@@ -30,7 +30,7 @@ struct ResArgs {
     const char *res; int64_t res_slab;   // the resident operand, K-blocked, the parts' slabs behind one another
     const char *str; int64_t str_slab;   // the other one
     const float *side;                   // what comes with 32 streaming rows.  G = 0: their bias (a float each; -inf behind the last class);
-                                         // G > 0: 128 words, log-sum-exp, weight, label (as they are needed) and 32 unused
+                                         // G > 0: 128 words, log-sum-exp, weight, label (as they are needed, weights over the scale of g) and 32 unused
     const int32_t *n_rows;
     int row0, max_rows;                  // the chunk: rows row0 .. row0 + max_rows of the list
     int class_tiles;                     // G = 0: the walk

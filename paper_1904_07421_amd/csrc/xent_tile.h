@@ -230,6 +230,7 @@ struct GradArgs {
     int H;
     void *out;
     float *acc;                     // dV over several chunks of rows
+    const float *scale;             // what g was divided by (gradients in bf16)
 };
 template <bool WEIGHTS, int WM>
 __device__ __forceinline__ GradPlan grad_plan(const GradArgs &a) {
@@ -299,6 +300,7 @@ __device__ __forceinline__ void grad_finish(const GradArgs &a, const GradPlan &g
     }
     const int64_t row = (WEIGHTS ? (int64_t)n : (int64_t)a.row_of[a.row0 + n]) * a.H;
     const bool more = WEIGHTS && *a.n_rows - a.row0 > a.max_rows;       // chunks to come
+    const float scale = sizeof(O) == 2 ? *a.scale : 1.0f;
 #pragma unroll
     for (int v = 0; v < 4; ++v) {
         const int m = m0 + v * 8, left = a.H - m < 4 ? a.H - m : 4;
@@ -312,7 +314,7 @@ __device__ __forceinline__ void grad_finish(const GradArgs &a, const GradPlan &g
         }
         O e[4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) e[k] = from_f32<O>(s[v][k]);
+        for (int k = 0; k < 4; ++k) e[k] = from_f32<O>(s[v][k] * scale);
         O *o = static_cast<O *>(a.out) + to;
         if (left == 4) {
             __builtin_memcpy(o, e, sizeof(e));
@@ -329,6 +331,7 @@ __device__ __forceinline__ void grad_finish(const GradArgs &a, const GradPlan &g
 struct BiasArgs {
     const float *part;
     float *db;
+    const float *scale;             // nullptr: 1
     int width, places;              // classes in whole blocks; resident_kernel's places
 };
 template <int WAVES>
@@ -345,6 +348,7 @@ __device__ __forceinline__ void bias_finish(const BiasArgs &b, const GradArgs &a
     if (q || c >= a.C) return;
 #pragma unroll
     for (int k = 1; k < WAVES; ++k) s += sums[k][l];
+    if (b.scale) s *= *b.scale;
     b.db[c] = a.row0 > 0 ? b.db[c] + s : s;
 }
 // Blocks take pieces in turn: how many there are depends on the number of rows, which the host does not know.

@@ -147,3 +147,63 @@ def test_a_mask_of_the_lowest_value_is_a_mask(dtype, H, C, grad):
         assert all(bool(t.isfinite().all()) for t in got[-1])
     for other in got[1:]:
         assert all(torch.equal(u, v) for u, v in zip(got[0], other))
+
+
+@pytest.mark.parametrize("weights", ["alike", "one row"])
+@pytest.mark.parametrize("n,H,C", [(40, 150, 3000), (2000, 512, 2500), (300, 600, 3000), (1500, 256, 4099)])
+def test_weights_that_are_alike_are_not_rounded(n, H, C, weights):
+    """Gradients in bf16 of improbable labels (p < 2^-9, so that p - 1 rounds to -1): the label's own derivative is then off by no more
+    than p of it, whatever the weight that all rows have, or the only row.  The other classes' are rounded, 2^-8 of each."""
+    import torch
+    import paper_1904_07421_amd as J
+    from oracle import head_oracle as O
+    from test_gpu_xent import _f32, _host, _i32, _to
+    print(f"xent weights n={n} H={H} C={C} {weights}", flush=True)
+    U32, UB = 2.0 ** -24, 2.0 ** -8
+    rng = np.random.default_rng([n, H, C])
+    h_t, h = _to(rng.uniform(-1, 1, (n, H)), "bf16")
+    V_t, V = _to(rng.standard_normal((C, H)) * 0.2 / np.sqrt(H), "bf16")
+    h, V = h.astype(np.float64), V.astype(np.float64)
+    label = rng.integers(0, C, n)
+    if weights == "one row":
+        label[np.arange(n) != n // 2] = -1
+    for w in (1.0 / 3, 0.0021019, -1.7e-5, 1.99):
+        gloss = np.full(n, w, np.float32)
+        _, lse = J.jitdb_softmax_xent_forward(h_t, V_t, _i32(label))
+        dh_t, dV_t, db_t = J.jitdb_softmax_xent_backward(h_t, V_t, _i32(label), lse, gloss=_f32(gloss), grad_dtype=torch.bfloat16)
+        dh, dV, db, g, p = O.softmax_xent_backward(h, V, None, label, gloss.astype(np.float64))
+        used = label != -1
+        own = np.zeros_like(p)
+        own[used, label[used]] = 1
+        assert (p[used, label[used]] < 2.0 ** -9).all()
+        size = np.abs(h) @ np.abs(V).T
+        rel = ((H + 4) * U32 * size).max() * 2 + (C + 4) * U32 + 2.0 ** -20 + 2.0 ** -22 * 16       # of a probability, as in the tests of sizes
+        g_err = abs(w) * (p * (rel + UB) * (1 + own))                                                # (p - 1 to -1 is off by p)
+        total = np.abs(g)
+        for name, t, want, err in (("dh", dh_t, dh, g_err @ np.abs(V) + (C + 8) * U32 * (total @ np.abs(V))),
+                                   ("dV", dV_t, dV, g_err.T @ np.abs(h) + (n + 8) * U32 * (total.T @ np.abs(h)))):
+            own_err = abs(w) * ((own * p) @ np.abs(V) if name == "dh" else (own * p).T @ np.abs(h))
+            most = (err + own_err) * (1 + UB) + UB * np.abs(want) + 1e-36
+            assert np.all(np.abs(_host(t) - want) <= most), (name, w, float((np.abs(_host(t) - want) / most).max()))
+        db_err = abs(w) * (p * rel).sum(0) + (n + 16) * U32 * total.sum(0)
+        assert np.all(np.abs(_host(db_t) - db) <= db_err + 1e-36), w
+
+
+def test_weights_of_any_size():
+    """Weights of every magnitude, 0 and none that counts: as the same call with fp32 gradients, rounded."""
+    import torch
+    import paper_1904_07421_amd as J
+    torch.manual_seed(2)
+    n, H, C = 700, 60, 300
+    h, V = torch.randn(n, H, device="cuda").bfloat16(), torch.randn(C, H, device="cuda").bfloat16()
+    label = torch.randint(-1, C, (n,), device="cuda", dtype=torch.int32)
+    for scale in (0.0, 1e-41, 1e-30, 1.0, 1e30):
+        gloss = torch.randn(n, device="cuda") * scale
+        gloss[::5] = 0
+        _, lse = J.jitdb_softmax_xent_forward(h, V, label)
+        a = J.jitdb_softmax_xent_backward(h, V, label, lse, gloss=gloss, grad_dtype=torch.bfloat16)
+        b = J.jitdb_softmax_xent_backward(h, V, label, lse, gloss=gloss)
+        for u, v in zip(a, b):
+            # products of rounded terms and a rounded result, as a norm (below the normal range nothing is promised)
+            assert float((u.double() - v.double()).norm()) <= 2.0 ** -7 * float(v.double().norm()) + 1e-34
+        assert not bool(a[0][::5].any())
